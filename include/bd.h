@@ -19,6 +19,13 @@
  *   bd_top1_ce             top-1 cross-entropy against the verifier (Eqs. 5-7)
  *   bd_sample_budgets      B ~ Cat(B, w) per training sample (Alg. 1)
  *
+ * and, over a KV cache held in 8 or 4 bits (bd_qkv_desc):
+ *
+ *   bd_cache_append_q      per-round cache growth, rows quantised as they are written
+ *   bd_cache_read_q        rows read back as bf16
+ *   bd_sparse_decode_attn_q  drafter attention over the selected entries
+ *   bd_verify_attn_q       verifier attention at the gamma+1 draft positions
+ *
  * Common conventions
  *   - Tensors are raw device pointers.  bf16 data are passed as uint16_t bit
  *     patterns; head_dim must be 128.
@@ -403,6 +410,107 @@ bd_status bd_top1_ce(const float* student, int64_t student_stride, const float* 
  * ---------------------------------------------------------------------- */
 bd_status bd_sample_budgets(const float* u, int32_t count, const int32_t* budgets, const float* weights, int32_t n,
                             int32_t* out, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * KV cache of one layer held in 8 or 4 bits.
+ *
+ * A row (one position of one KV head) of K or of V is
+ *   - 128 codes: e4m3 bytes (bits = 8), or e2m1, two to a byte, the even element
+ *     in the low half (bits = 4, 64 bytes);
+ *   - 4 scale bytes, one per block of 32 elements (element d: block d / 32).
+ * An element's value is its code's value times 2^(scale byte - 127); a block of
+ * scale byte 255 is not a number (the microscaling formats MXFP8 and MXFP4).
+ * Every value that bd_cache_append_q writes is exact in bf16.
+ *
+ * Rows are numbered; row r's codes are at r * (16 * bits) bytes and its scales
+ * at 4 * r bytes of their arrays, in K and V alike.  Strides count rows:
+ * contiguous: row(s, g, t) = s*stride_seq + g*stride_head + t*stride_tok;
+ * paged: row(s, g, t) = page_table[s*max_pages_per_seq + t/page_size]*stride_page
+ *   + g*stride_head + (t % page_size)*stride_tok.
+ * Page numbers, lengths and the causal rule are those of bd_kv_desc.  Page
+ * sizes that are multiples of 16 are read through one table entry per page.
+ * Limits (BD_ERR_UNSUPPORTED beyond): 2^31 - 1 rows, stride_tok of 2^19 rows. */
+typedef struct bd_qkv_desc {
+  uint8_t* k;                 /* codes, 16-byte aligned; only bd_cache_append_q writes */
+  uint8_t* v;
+  uint8_t* k_scale;           /* scale bytes, 4-byte aligned */
+  uint8_t* v_scale;
+  int32_t bits;               /* 8 or 4 */
+  int32_t num_seqs;           /* S >= 1 */
+  int32_t num_kv_heads;       /* Hkv >= 1 */
+  int32_t head_dim;           /* must be 128 */
+  int32_t max_seq_len;        /* host bound: every seq_lens[s] <= max_seq_len */
+  int32_t page_size;          /* paged: tokens per page (>= 1) */
+  int32_t max_pages_per_seq;  /* paged: max_seq_len <= max_pages_per_seq * page_size */
+  int32_t num_pages;          /* paged: pages in the pool */
+  int32_t* seq_lens;          /* device [S]: L_s, clamped to [0, max_seq_len]; only bd_cache_append_q writes */
+  const int32_t* page_table;  /* NULL, or device [S][max_pages_per_seq] page numbers */
+  int64_t stride_seq;         /* rows; contiguous layout only */
+  int64_t stride_head;
+  int64_t stride_tok;
+  int64_t stride_page;        /* rows; paged only */
+} bd_qkv_desc;
+
+/* ------------------------------------------------------------------------
+ * bd_cache_append_q -- append rows to a quantised cache (bd_cache_append's
+ * operation; Alg. 2's cache update).
+ *
+ * For every sequence s, its new rows go to positions L_s .., quantised as they
+ * are written; rows at or past max_seq_len are dropped, and so are rows whose
+ * page is outside the pool; seq_lens is advanced in place by the rows below
+ * max_seq_len.  No other byte of the cache changes.
+ * With a = max|x| over a block of 32 elements and E = floor(log2 a), the block's
+ * exponent is e = E - emax, or one more when a > top * 2^E (emax = 8, top =
+ * 1.8125 for 8 bits; 2, 1.75 for 4), clamped to [-111, 127 - emax] (-111 for
+ * a = 0): the smallest at which the maximum saturates by no more than half a
+ * step.  The scale byte is e + 127 and each code is x * 2^-e rounded to nearest,
+ * ties to even, saturating at 448 (8 bits) or 6 (4 bits).  A block with a NaN or
+ * an infinity gets scale byte 255 and zero codes.
+ * k_new, v_new [S][n][Hkv][128] bf16, 16-byte aligned.
+ * counts     NULL (n rows for every sequence), or device [S]: sequence s gets its
+ *            first counts[s] rows (clamped to [0, n]).
+ * idx, nsel  as in bd_cache_append (NULL, or the sparse list, appended in place).
+ * One launch on `stream` up to n = 16, else two.  n up to 2^30.
+ * ---------------------------------------------------------------------- */
+bd_status bd_cache_append_q(const bd_qkv_desc* kv, const uint16_t* k_new, const uint16_t* v_new, int32_t n,
+                            const int32_t* counts, int32_t* idx, int32_t ld_idx, int32_t* nsel, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * bd_cache_read_q -- rows of a quantised cache read back as bf16, for the
+ * operations that take a bf16 cache (selection, the multi-view block).
+ *
+ * Output row i of (s, g) is the value of position first[s] + i where that lies
+ * in [0, L_s) and its page in the pool, and zero elsewhere.
+ * first      NULL (0), or device [S].
+ * k_out, v_out  bf16, element (s, g, i, d) at s*out_stride_seq + g*out_stride_head
+ *            + i*out_stride_tok + d; 16-byte aligned; either may be NULL.  Strides
+ *            are non-negative multiples of 8 elements.  n up to 2^30.
+ * ---------------------------------------------------------------------- */
+bd_status bd_cache_read_q(const bd_qkv_desc* kv, const int32_t* first, int32_t n, uint16_t* k_out, uint16_t* v_out,
+                          int64_t out_stride_seq, int64_t out_stride_head, int64_t out_stride_tok, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * bd_sparse_decode_attn_q, bd_verify_attn_q -- bd_sparse_decode_attn and
+ * bd_verify_attn over a quantised cache: the same arguments, shapes, visibility
+ * and outputs, of the cache's values.  Scores, softmax and sums are fp32; the
+ * softmax weights enter the sum of values in bf16, normalised by the sum of the
+ * same rounded weights.  Keys that a row does not see (past the length, later
+ * drafts, absent entries) do not reach it, whatever their bytes hold; a value
+ * that is not a number reaches the outputs of the rows that see it.
+ * The work is divided by the lengths on the device, so that capacity beyond
+ * them and uneven lengths cost nothing; results do not depend on scheduling.
+ * ---------------------------------------------------------------------- */
+size_t bd_sparse_decode_attn_q_workspace_bytes(int32_t num_seqs, int32_t num_kv_heads, int32_t num_q_heads,
+                                               int32_t ld_idx);
+bd_status bd_sparse_decode_attn_q(const bd_qkv_desc* kv, const uint16_t* q, int32_t num_q_heads,
+                                  const int32_t* idx, int32_t ld_idx, const int32_t* nsel, float scale,
+                                  uint16_t* out, float* lse_out,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+size_t bd_verify_attn_q_workspace_bytes(int32_t num_seqs, int32_t num_kv_heads, int32_t num_q_heads,
+                                        int32_t gamma, int32_t max_seq_len);
+bd_status bd_verify_attn_q(const bd_qkv_desc* kv, const uint16_t* q, int32_t num_q_heads, int32_t gamma, float scale,
+                           uint16_t* out, float* lse_out,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

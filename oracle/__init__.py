@@ -26,4 +26,8 @@ from .bd_oracle import (  # noqa: F401
     top1_ce,
     budget_thresholds,
     sample_budgets,
+    mx_grid,
+    mx_quantise,
+    mx_values,
+    cache_append_q,
 )

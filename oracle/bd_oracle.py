@@ -618,3 +618,82 @@ def sample_budgets(u, budgets, weights) -> np.ndarray:
             j += 1
         out[i] = budgets[j]
     return out
+
+
+# --------------------------------------------------------------------------
+# Caches held in 8 or 4 bits (microscaling formats: blocks of 32 with a power-of-two scale)
+# --------------------------------------------------------------------------
+
+def mx_grid(bits: int) -> np.ndarray:
+    """The format's non-negative values in ascending order; value i has code i (the sign bit aside)."""
+    if bits == 4:
+        return np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+    sub = np.arange(8) / 512.0                                     # multiples of 2^-9
+    nrm = [(1.0 + m / 8.0) * 2.0 ** (k - 7) for k in range(1, 16) for m in range(8)]
+    return np.concatenate([sub, nrm])[:127]                        # code 127 is not a number
+
+
+def mx_quantise(x, bits: int):
+    """Rows x [...][128] (bf16 bits) -> codes uint8 [...][128 or 64] and scale bytes uint8 [...][4].
+
+    Block exponent: the smallest e at which max|x| 2^-e is at most half a step above the largest value, within
+    [-111, 127 - floor(log2 of the largest value)], -111 for a block of zeros.  Codes: the nearest value of x 2^-e
+    (even code on a tie, the largest at most).  A block that holds a NaN or an infinity: scale byte 255, zero codes.
+    4 bits: two codes to a byte, the even element in the low half.
+    """
+    grid = mx_grid(bits)
+    top = int(np.floor(np.log2(grid[-1])))
+    half = grid[-1] + (grid[-1] - grid[-2]) / 2
+    x = np.asarray(x, dtype=np.uint16)
+    v = bf16_to_f64(x).reshape(*x.shape[:-1], 4, 32)
+    sign = (x >> 15).reshape(v.shape)
+    bad = ~np.isfinite(v).all(-1)
+    a = np.where(bad, 0.0, np.abs(np.where(np.isfinite(v), v, 0.0)).max(-1))
+    e = np.full(a.shape, -111)
+    for cand in range(-111, 127 - top + 1):                        # ascending: each step keeps what fits already
+        e = np.where(a * 2.0 ** -e.astype(np.float64) > half, cand, e)
+    y = np.abs(np.where(bad[..., None], 0.0, v)) * 2.0 ** -e.astype(np.float64)[..., None]
+    edges = (grid[1:] + grid[:-1]) / 2
+    lo = np.searchsorted(edges, y, side="left")                    # an element on an edge: the lower value
+    on_edge = (lo < edges.size) & (y == edges[np.minimum(lo, edges.size - 1)])
+    code = lo + (on_edge & (lo % 2 == 1))
+    code = np.where(bad[..., None], 0, code + (sign.astype(np.int64) << (bits - 1)))
+    code = code.reshape(x.shape).astype(np.uint8)
+    if bits == 4:
+        code = code[..., 0::2] | (code[..., 1::2] << 4)
+    return code, np.where(bad, 255, e + 127).astype(np.uint8)
+
+
+def mx_values(codes, scales, bits: int) -> np.ndarray:
+    """float64 values [...][128] of codes and scale bytes (NaN for a block of scale byte 255 and for e4m3's NaN code)."""
+    codes, scales = np.asarray(codes, np.uint8), np.asarray(scales, np.uint8)
+    if bits == 4:
+        codes = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], 128)
+    pos = mx_grid(bits)
+    if bits == 8:
+        pos = np.append(pos, np.nan)
+    table = np.concatenate([pos, -pos])
+    two = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return table[codes] * np.repeat(two, 32, axis=-1)
+
+
+def cache_append_q(cache, seq_lens, k_new, v_new, bits: int, counts=None, idx=None, nsel=None):
+    """cache_append on a quantised cache (k, v, k_scale, v_scale), each [S][Hkv][cap][bytes of a row]: sequence s gets
+    its first counts[s] new rows (all by default).  Returns (cache, seq_lens[, idx, nsel])."""
+    n = k_new.shape[1]
+    parts = mx_quantise(k_new, bits) + mx_quantise(v_new, bits)
+    new = (parts[0], parts[2], parts[1], parts[3])
+    out, lens = [np.array(b, copy=True) for b in cache], np.array(seq_lens, np.int32, copy=True)
+    if idx is not None:
+        idx, nsel = np.array(idx, np.int32, copy=True), np.array(nsel, np.int32, copy=True)
+    for s in range(len(lens)):
+        c = n if counts is None else min(max(int(counts[s]), 0), n)
+        w = max(0, min(c, out[0].shape[2] - int(lens[s])))
+        for buf, rows in zip(out, new):
+            buf[s, :, lens[s]:lens[s] + w] = rows[s, :w].transpose(1, 0, 2)
+        if idx is not None:
+            a = min(w, idx.shape[2] - int(nsel[s]))
+            idx[s, :, nsel[s]:nsel[s] + a] = np.arange(lens[s], lens[s] + a)
+            nsel[s] += a
+        lens[s] += w
+    return (tuple(out), lens) if idx is None else (tuple(out), lens, idx, nsel)

@@ -10,11 +10,16 @@ Functions carry the names of the C entry points:
 
     bd_select_kv, bd_select_kv_chunks, bd_sparse_decode_attn,
     bd_multiview_attn, bd_multiview_attn_bwd, bd_verify_attn, bd_verify_attn_noalloc, bd_accept_len,
-    bd_cache_append, bd_cache_rollback, bd_top1_ce, bd_sample_budgets
+    bd_cache_append, bd_cache_rollback, bd_top1_ce, bd_sample_budgets,
+    bd_cache_append_q, bd_cache_read_q, bd_sparse_decode_attn_q, bd_verify_attn_q
 
 KV caches are bf16 tensors, either contiguous ``[S][Hkv][L][128]`` or paged
 ``[num_pages][Hkv][page_size][128]`` together with an int32 ``page_table``
 ``[S][max_pages]``.  ``seq_lens`` is an int32 device tensor ``[S]``.
+
+The ``_q`` operations take a cache held in 8 or 4 bits instead, a ``QuantKV`` of
+uint8 tensors of the same layouts: codes with 128 (8 bits) or 64 (4 bits) bytes
+a row, and 4 scale bytes a row (``quant_kv_empty`` makes one).
 """
 from __future__ import annotations
 
@@ -24,7 +29,7 @@ import math
 import os
 import struct
 import threading
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -33,6 +38,8 @@ __all__ = [
     "bd_select_kv", "bd_select_kv_chunks", "bd_sparse_decode_attn", "bd_multiview_attn", "bd_multiview_attn_bwd", "bd_verify_attn",
     "bd_verify_attn_noalloc", "bd_accept_len",
     "bd_cache_append", "bd_cache_rollback", "bd_top1_ce", "bd_sample_budgets",
+    "QuantKV", "quant_kv_empty", "qkv_desc",
+    "bd_cache_append_q", "bd_cache_read_q", "bd_sparse_decode_attn_q", "bd_verify_attn_q",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -59,11 +66,25 @@ class KvDesc(ctypes.Structure):
     ]
 
 
+class QkvDesc(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("bits", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("max_pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("seq_lens", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+        ("stride_seq", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
+        ("stride_page", ctypes.c_int64),
+    ]
+
+
 _P = ctypes.c_void_p
 _I32, _I64, _F32, _SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
-_KV = ctypes.POINTER(KvDesc)
+_KV, _QKV = ctypes.POINTER(KvDesc), ctypes.POINTER(QkvDesc)
 _KV_BYTES = struct.Struct("@PPiiiiPqqqPiiiq")
 assert _KV_BYTES.size == ctypes.sizeof(KvDesc)
+_QKV_BYTES = struct.Struct("@PPPPiiiiiiiiPPqqqq")
+assert _QKV_BYTES.size == ctypes.sizeof(QkvDesc)
 _BF16, _I32T, _F32T = torch.bfloat16, torch.int32, torch.float32
 
 _SIGNATURES = {
@@ -90,6 +111,12 @@ _SIGNATURES = {
     "bd_verify_attn_noalloc": (_I32, [_KV, _P, _I32, _I32, _F32, _P, _P, _P]),
     "bd_accept_len_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
     "bd_accept_len": (_I32, [_P, _I64, _P, _I32, _I32, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "bd_cache_append_q": (_I32, [_QKV, _P, _P, _I32, _P, _P, _I32, _P, _P]),
+    "bd_cache_read_q": (_I32, [_QKV, _P, _I32, _P, _P, _I64, _I64, _I64, _P]),
+    "bd_sparse_decode_attn_q_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32]),
+    "bd_sparse_decode_attn_q": (_I32, [_QKV, _P, _I32, _P, _I32, _P, _F32, _P, _P, _P, _SZ, _P]),
+    "bd_verify_attn_q_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32, _I32]),
+    "bd_verify_attn_q": (_I32, [_QKV, _P, _I32, _I32, _F32, _P, _P, _P, _SZ, _P]),
 }
 
 _lib = None
@@ -102,12 +129,12 @@ def lib() -> ctypes.CDLL:
     return _lib if _lib is not None else _load()
 
 
-def _bind(kv_type) -> ctypes.CDLL:
+def _bind(kv_type, qkv_type) -> ctypes.CDLL:
     handle = ctypes.CDLL(library_path)
     for name, (res, args) in _SIGNATURES.items():
         fn = getattr(handle, name)
         fn.restype = res
-        fn.argtypes = [kv_type if a is _KV else a for a in args]
+        fn.argtypes = [kv_type if a is _KV else qkv_type if a is _QKV else a for a in args]
     return handle
 
 
@@ -118,8 +145,8 @@ def _load() -> ctypes.CDLL:
             if not os.path.exists(library_path):
                 raise BdError(BD_ERR_DEVICE, f"{library_path} is not built; run `python -m paper_2606_00144_amd.build`")
             # a CDLL of its own holds its own prototypes over the one loaded library
-            _packed = _bind(ctypes.c_char_p)
-            _lib = _bind(_KV)
+            _packed = _bind(ctypes.c_char_p, ctypes.c_char_p)
+            _lib = _bind(_KV, _QKV)
     return _lib
 
 
@@ -543,3 +570,184 @@ def bd_sample_budgets(u: torch.Tensor, budgets, weights) -> torch.Tensor:
     _check(lib().bd_sample_budgets(u.data_ptr(), u.numel(), ctypes.cast(b, ctypes.c_void_p),
                                    ctypes.cast(w, ctypes.c_void_p), n, out.data_ptr(), _stream()))
     return out
+
+
+# --------------------------------------------------------------------- caches held in 8 or 4 bits
+
+class QuantKV(NamedTuple):
+    """A KV cache held in 8 or 4 bits: uint8 codes [S, Hkv, L, 128 or 64] (contiguous) or
+    [num_pages, Hkv, page_size, 128 or 64] (paged) and uint8 scales of the same rows, [.., .., .., 4].  K and V
+    share strides, and the scales' strides are the codes' in rows (bd_qkv_desc describes the format)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def quant_kv_empty(n: int, num_kv_heads: int, rows: int, bits: int, device="cuda") -> QuantKV:
+    """An uninitialised cache of `bits` bits: n sequences of `rows` positions, or n pages of `rows`."""
+    _require(bits in (8, 4), "bits must be 8 or 4")
+    e = lambda w: torch.empty((n, num_kv_heads, rows, w), dtype=torch.uint8, device=device)
+    return QuantKV(e(16 * bits), e(16 * bits), e(4), e(4))
+
+
+_U8 = torch.uint8
+
+
+def _qkv(cache, seq_lens, page_table=None, max_seq_len=None):
+    """The bytes of a QkvDesc for these tensors (checked), and its (num_seqs, num_kv_heads, max_seq_len)."""
+    k, v, ks, vs = cache
+    sh, st = k.shape, k.stride()
+    if not (k.dtype == _U8 and len(sh) == 4 and (sh[3] == 128 or sh[3] == 64) and st[3] == 1):
+        raise BdError(BD_ERR_INVALID_ARG, "k must be uint8 codes [*, Hkv, *, 128 or 64] with a contiguous last dimension")
+    if not (v.dtype == _U8 and v.shape == sh and v.stride() == st):
+        raise BdError(BD_ERR_INVALID_ARG, "v must match k in shape and strides")
+    w, (n0, hkv, n2, _) = sh[3], sh
+    if not (ks.dtype == _U8 and vs.dtype == _U8 and ks.shape == (n0, hkv, n2, 4) and vs.shape == ks.shape
+            and ks.stride(3) == 1 and vs.stride() == ks.stride()):
+        raise BdError(BD_ERR_INVALID_ARG, "k_scale and v_scale must be uint8 [*, Hkv, *, 4] with equal strides")
+    rows = (st[0] // w, st[1] // w, st[2] // w)
+    sst = ks.stride()
+    for i in (0, 1, 2):          # a dimension of one has no stride to speak of
+        if sh[i] > 1 and not (st[i] % w == 0 and sst[i] == 4 * rows[i]):
+            raise BdError(BD_ERR_INVALID_ARG, "code and scale strides must be the same whole numbers of rows")
+    ls = seq_lens.shape
+    if not (seq_lens.dtype == _I32T and len(ls) == 1 and seq_lens.is_contiguous()):
+        raise BdError(BD_ERR_INVALID_ARG, "seq_lens must be contiguous int32 [S]")
+    S = ls[0]
+    if page_table is None:
+        if n0 != S:
+            raise BdError(BD_ERR_INVALID_ARG, "contiguous k must be [S, Hkv, L, 128 or 64]")
+        L = n2 if max_seq_len is None else int(max_seq_len)
+        if L > n2:
+            raise BdError(BD_ERR_INVALID_ARG, "max_seq_len exceeds the cache's rows")
+        geom = (0, 0, 0, seq_lens.data_ptr(), 0, rows[0], rows[1], rows[2], 0)
+    else:
+        ps = page_table.shape
+        if not (page_table.dtype == _I32T and len(ps) == 2 and ps[0] == S and page_table.is_contiguous()):
+            raise BdError(BD_ERR_INVALID_ARG, "page_table must be contiguous int32 [S, max_pages]")
+        L = ps[1] * n2 if max_seq_len is None else int(max_seq_len)
+        geom = (n2, ps[1], n0, seq_lens.data_ptr(), page_table.data_ptr(), 0, rows[1], rows[2], rows[0])
+    try:
+        return _QKV_BYTES.pack(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), w // 16, S, hkv, HEAD_DIM, L,
+                               *geom), S, hkv, L
+    except struct.error:
+        raise BdError(BD_ERR_UNSUPPORTED, "a size of the cache is beyond 32 bits") from None
+
+
+def qkv_desc(cache: QuantKV, seq_lens: torch.Tensor, page_table: Optional[torch.Tensor] = None,
+             max_seq_len: Optional[int] = None) -> QkvDesc:
+    """Describe a quantised KV cache for the C ABI (tensors must outlive the call)."""
+    return QkvDesc.from_buffer_copy(_qkv(cache, seq_lens, page_table, max_seq_len)[0])
+
+
+def _here(*tensors) -> None:
+    """Every tensor (None aside) lies on the current GPU, whose stream the call is issued on."""
+    dev = _get_device() if _get_device is not None and torch.cuda.is_initialized() else 0
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise BdError(BD_ERR_INVALID_ARG, f"tensors must be on the current GPU ({dev}), not on {t.device}")
+
+
+def _ws_q(op: str, nbytes: int, like: torch.Tensor, stream: int, workspace: Optional[Workspace]):
+    """As _ws, but a graph under capture gets scratch of its own (cleared by the graph itself) unless the caller
+    gives a workspace: two graphs that shared a default one could be replayed side by side."""
+    if workspace is None and torch.cuda.is_current_stream_capturing():
+        workspace = Workspace()
+    return _ws(op, nbytes, like, stream, workspace)
+
+
+def bd_cache_append_q(cache: QuantKV, seq_lens: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, *,
+                      counts: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None,
+                      nsel: Optional[torch.Tensor] = None, page_table: Optional[torch.Tensor] = None,
+                      max_seq_len: Optional[int] = None) -> None:
+    """Append rows in place, quantised as they are written: k_new, v_new bf16 [S, n, Hkv, 128] go to positions
+    seq_lens[s] .. (the first counts[s] of them with counts int32 [S]); seq_lens (and, with the sparse list
+    idx [S, Hkv, ld] / nsel [S], the list) advance in place."""
+    kv, S, hkv, _ = _qkv(cache, seq_lens, page_table, max_seq_len)
+    ns = k_new.shape
+    _require(k_new.dtype == _BF16 and len(ns) == 4 and k_new.is_contiguous() and v_new.shape == ns and v_new.is_contiguous()
+             and v_new.dtype == _BF16 and ns[0] == S and ns[2] == hkv and ns[3] == HEAD_DIM,
+             "k_new and v_new must be contiguous bf16 [S,n,Hkv,128]")
+    _require(counts is None or (counts.dtype == _I32T and counts.shape == (S,) and counts.is_contiguous()), "counts must be int32 [S]")
+    _require((idx is None) == (nsel is None), "idx and nsel go together")
+    ld = 0
+    if idx is not None:
+        ld = idx.shape[-1]
+        _require(idx.dtype == _I32T and idx.shape == (S, hkv, ld) and idx.is_contiguous(), "idx must be contiguous int32 [S,Hkv,ld]")
+        _require(nsel.dtype == _I32T and nsel.shape == (S,) and nsel.is_contiguous(), "nsel must be int32 [S]")
+    _here(*cache, seq_lens, k_new, v_new, counts, idx, nsel, page_table)
+    _check(_packed_lib().bd_cache_append_q(kv, k_new.data_ptr(), v_new.data_ptr(), ns[1], _ptr(counts), _ptr(idx), ld,
+                                           _ptr(nsel), _stream()))
+
+
+def bd_cache_read_q(cache: QuantKV, seq_lens: torch.Tensor, n: int, *, first: Optional[torch.Tensor] = None,
+                    with_v: bool = True, page_table: Optional[torch.Tensor] = None, max_seq_len: Optional[int] = None,
+                    outputs=None):
+    """Rows first[s] .. first[s]+n-1 (first None: 0) of every (sequence, KV head) as bf16 (k, v) [S, Hkv, n, 128]; rows
+    that the cache does not hold are zero.  with_v=False: (k, None), as the selections need.  outputs: optional
+    preallocated (k, v), of equal strides with a contiguous last dimension (a part of a larger bf16 cache, say)."""
+    kv, S, hkv, _ = _qkv(cache, seq_lens, page_table, max_seq_len)
+    _require(n >= 0, "n must not be negative")
+    _require(first is None or (first.dtype == _I32T and first.shape == (S,) and first.is_contiguous()), "first must be int32 [S]")
+    shape = (S, hkv, n, HEAD_DIM)
+    ko, vo = (tuple(outputs) + (None, None))[:2] if outputs is not None else (None, None)
+    if ko is None:
+        ko = cache[0].new_empty(shape, dtype=_BF16)
+    if not with_v:
+        vo = None
+    elif vo is None:
+        vo = torch.empty_strided(shape, ko.stride(), dtype=_BF16, device=ko.device)
+    st = ko.stride()
+    _require(ko.dtype == _BF16 and ko.shape == shape and st[3] == 1, "k output must be bf16 [S,Hkv,n,128]")
+    _require(vo is None or (vo.dtype == _BF16 and vo.shape == shape and vo.stride() == st), "v output must match k's")
+    _here(*cache, seq_lens, first, ko, vo, page_table)
+    _check(_packed_lib().bd_cache_read_q(kv, _ptr(first), n, ko.data_ptr(), _ptr(vo), st[0], st[1], st[2], _stream()))
+    return ko, vo
+
+
+def bd_sparse_decode_attn_q(cache: QuantKV, q: torch.Tensor, idx: torch.Tensor, nsel: torch.Tensor, seq_lens: torch.Tensor,
+                            *, scale: Optional[float] = None, return_lse: bool = False,
+                            page_table: Optional[torch.Tensor] = None, max_seq_len: Optional[int] = None,
+                            out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                            workspace: Optional[Workspace] = None):
+    """Drafter decode attention over selected entries of a quantised cache.  q: bf16 [S, Hq, 128]; idx int32
+    [S, Hkv, ld].  out / lse: optional preallocated outputs."""
+    kv, S, hkv, _ = _qkv(cache, seq_lens, page_table, max_seq_len)
+    qs, xs = q.shape, idx.shape
+    if not (q.dtype == _BF16 and len(qs) == 3 and q.is_contiguous() and qs[0] == S and qs[2] == HEAD_DIM):
+        raise BdError(BD_ERR_INVALID_ARG, "q must be contiguous bf16 [S,Hq,128]")
+    if not (idx.dtype == _I32T and len(xs) == 3 and idx.is_contiguous() and xs[0] == S and xs[1] == hkv):
+        raise BdError(BD_ERR_INVALID_ARG, "idx must be contiguous int32 [S,Hkv,ld]")
+    if not (nsel.dtype == _I32T and nsel.shape == (S,) and nsel.is_contiguous()):
+        raise BdError(BD_ERR_INVALID_ARG, "nsel must be int32 [S]")
+    Hq, ld = qs[1], xs[2]
+    out = _out_like(out, q, "out")
+    lse = _out(lse, (S, Hq), _F32T, q, "lse") if return_lse else None
+    _here(*cache, q, idx, nsel, seq_lens, page_table, out, lse)
+    stream = _stream()
+    wp, wb = _ws_q("decode_q", _ws_bytes("bd_sparse_decode_attn_q_workspace_bytes", S, hkv, Hq, ld), q, stream, workspace)
+    _check(_packed_lib().bd_sparse_decode_attn_q(kv, q.data_ptr(), Hq, idx.data_ptr(), ld, nsel.data_ptr(), _scale(scale),
+                                                 out.data_ptr(), _ptr(lse), wp, wb, stream))
+    return (out, lse) if return_lse else out
+
+
+def bd_verify_attn_q(cache: QuantKV, q: torch.Tensor, seq_lens: torch.Tensor, *, scale: Optional[float] = None,
+                     return_lse: bool = False, page_table: Optional[torch.Tensor] = None,
+                     max_seq_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, workspace: Optional[Workspace] = None):
+    """Verifier attention at the gamma+1 draft positions over a quantised cache.  q: bf16 [S, gamma+1, Hq, 128]
+    (gamma = 0: a single-token decode over the whole cache).  out / lse: optional preallocated outputs."""
+    kv, S, hkv, L = _qkv(cache, seq_lens, page_table, max_seq_len)
+    qs = q.shape
+    if not (q.dtype == _BF16 and len(qs) == 4 and q.is_contiguous() and qs[0] == S and qs[3] == HEAD_DIM):
+        raise BdError(BD_ERR_INVALID_ARG, "q must be contiguous bf16 [S,gamma+1,Hq,128]")
+    _, R, Hq, _ = qs
+    out = _out_like(out, q, "out")
+    lse = _out(lse, (S, R, Hq), _F32T, q, "lse") if return_lse else None
+    _here(*cache, q, seq_lens, page_table, out, lse)
+    stream = _stream()
+    wp, wb = _ws_q("verify_q", _ws_bytes("bd_verify_attn_q_workspace_bytes", S, hkv, Hq, R - 1, L), q, stream, workspace)
+    _check(_packed_lib().bd_verify_attn_q(kv, q.data_ptr(), Hq, R - 1, _scale(scale), out.data_ptr(), _ptr(lse), wp, wb,
+                                          stream))
+    return (out, lse) if return_lse else out

@@ -45,6 +45,16 @@ __device__ inline void dma16_hidden(const uint16_t* base, uint32_t voff, uint32_
       : "s"(lds), "v"(voff), "s"(base)
       : "memory", "m0");
 }
+// One 4-byte load a lane: lane l's bytes land at the LDS address + 4*l.
+__device__ inline void dma4_hidden(const void* g, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n"
+      "s_nop 0\n"
+      "global_load_lds_dword %1, off"
+      :
+      : "s"(lds), "v"(g)
+      : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // Where tiles are read by rows alone (scores): chunk c (16 bytes) of row m of a 16-row sub-tile sits at position

@@ -13,6 +13,7 @@
 
 #include "bd.h"
 #include "bd_kernels.hpp"
+#include "quant.hpp"
 
 namespace {
 
@@ -629,6 +630,180 @@ bd_status bd_sample_budgets(const float* u, int32_t count, const int32_t* budget
   for (int i = 0; i < n; ++i) t.thr[i] = t.thr[i] / acc;
   if (count == 0) return BD_OK;
   return launched(bd::launch_sample(u, count, t, out, stream));
+}
+
+// ---------------------------------------------------------------- quantised caches
+namespace {
+// Rows of the layout, its largest row number plus one.
+int64_t q_rows(const bd_qkv_desc* kv) {
+  if (kv->page_table)
+    return (int64_t)(kv->num_pages - 1) * kv->stride_page + (int64_t)(kv->num_kv_heads - 1) * kv->stride_head +
+           (int64_t)(kv->page_size - 1) * kv->stride_tok + 1;
+  const int64_t L = kv->max_seq_len > 0 ? kv->max_seq_len : 1;
+  return (int64_t)(kv->num_seqs - 1) * kv->stride_seq + (int64_t)(kv->num_kv_heads - 1) * kv->stride_head +
+         (L - 1) * kv->stride_tok + 1;
+}
+
+// Checks shared by every operation on a quantised cache.
+bd_status check_qkv(const bd_qkv_desc* kv, bool need_k, bool need_v, int32_t num_q_heads) {
+  if (!kv) return fail(BD_ERR_INVALID_ARG, "kv descriptor is NULL");
+  if (kv->head_dim != BD_HEAD_DIM) return fail(BD_ERR_UNSUPPORTED, "head_dim %d is not 128", kv->head_dim);
+  if (kv->bits != 8 && kv->bits != 4) return fail(BD_ERR_UNSUPPORTED, "bits %d is neither 8 nor 4", kv->bits);
+  if ((need_k && (!kv->k || !kv->k_scale)) || (need_v && (!kv->v || !kv->v_scale)))
+    return fail(BD_ERR_INVALID_ARG, "a code or scale pointer is NULL");
+  if ((need_k && (!aligned(kv->k, 16) || !aligned(kv->k_scale, 4))) ||
+      (need_v && (!aligned(kv->v, 16) || !aligned(kv->v_scale, 4))))
+    return fail(BD_ERR_INVALID_ARG, "codes must be 16-byte aligned, scales 4-byte aligned");
+  if (!kv->seq_lens) return fail(BD_ERR_INVALID_ARG, "seq_lens is NULL");
+  if (kv->num_seqs < 1 || kv->num_kv_heads < 1) return fail(BD_ERR_INVALID_ARG, "num_seqs and num_kv_heads must be >= 1");
+  if (kv->max_seq_len < 0) return fail(BD_ERR_INVALID_ARG, "max_seq_len < 0");
+  if (num_q_heads < 1 || num_q_heads % kv->num_kv_heads != 0)
+    return fail(BD_ERR_INVALID_ARG, "num_q_heads %d is not a positive multiple of num_kv_heads %d", num_q_heads,
+                kv->num_kv_heads);
+  if ((int64_t)kv->num_seqs * kv->num_kv_heads > kMaxPairs || num_q_heads / kv->num_kv_heads > kMaxGroup)
+    return fail(BD_ERR_UNSUPPORTED, "more than 2^24 (sequence, KV head) pairs or 2^16 query heads per KV head");
+  const int64_t far = (int64_t)1 << 31;                       // no stride of a layout of fewer rows is larger
+  if (kv->stride_head < 0 || kv->stride_tok < 0 || (kv->page_table ? kv->stride_page : kv->stride_seq) < 0)
+    return fail(BD_ERR_INVALID_ARG, "strides must not be negative");
+  if (kv->stride_head >= far || kv->stride_tok > (1 << 19) || (kv->page_table ? kv->stride_page : kv->stride_seq) >= far)
+    return fail(BD_ERR_UNSUPPORTED, "a stride above 2^31 - 1 rows, or stride_tok above 2^19");
+  if (kv->page_table) {
+    if (kv->page_size < 1 || kv->max_pages_per_seq < 1 || kv->num_pages < 1)
+      return fail(BD_ERR_INVALID_ARG, "paged layout needs page_size, max_pages_per_seq and num_pages >= 1");
+    if ((int64_t)kv->max_seq_len > (int64_t)kv->max_pages_per_seq * kv->page_size)
+      return fail(BD_ERR_INVALID_ARG, "max_seq_len exceeds max_pages_per_seq * page_size");
+  }
+  if (q_rows(kv) > INT32_MAX) return fail(BD_ERR_UNSUPPORTED, "the layout spans more than 2^31 - 1 rows");
+  return BD_OK;
+}
+
+bd::QView make_qview(const bd_qkv_desc& d) {
+  bd::QView v{};
+  v.k = d.k; v.v = d.v; v.k_scale = d.k_scale; v.v_scale = d.v_scale;
+  v.seq_lens = d.seq_lens; v.page_table = d.page_table;
+  v.stride_seq = d.stride_seq; v.stride_head = d.stride_head; v.stride_tok = d.stride_tok; v.stride_page = d.stride_page;
+  v.num_seqs = d.num_seqs; v.num_kv_heads = d.num_kv_heads; v.max_seq_len = d.max_seq_len;
+  v.page_size = d.page_size; v.max_pages_per_seq = d.max_pages_per_seq; v.num_pages = d.num_pages;
+  return v;
+}
+
+bd_status run_qattn(const bd_qkv_desc* kv, const uint16_t* q, int32_t Hq, int32_t nq, const int32_t* idx,
+                    int32_t ld_idx, const int32_t* nsel, bool gather, float scale, uint16_t* out, float* lse, void* ws,
+                    size_t ws_bytes, hipStream_t stream) {
+  const bd::QAttnPlan pl = bd::plan_qattn(kv->num_seqs, kv->num_kv_heads, Hq, nq, gather ? ld_idx : kv->max_seq_len,
+                                          gather, kv->page_table != nullptr, kv->page_table ? kv->page_size : 0);
+  if (pl.nblk < 0) return fail(BD_ERR_UNSUPPORTED, "problem too large for one launch");
+  const bd_status st = check_ws(ws, ws_bytes, pl.ws_bytes);
+  if (st != BD_OK) return st;
+  bd::QAttnParams p{};
+  p.kv = make_qview(*kv);
+  p.q = q;
+  p.out = out;
+  p.lse = lse;
+  p.idx = gather ? (idx ? idx : nsel) : nullptr;   // non-NULL: gathered (an empty list is never read)
+  p.nsel = nsel;
+  p.ld_idx = ld_idx;
+  p.S = kv->num_seqs;
+  p.Hkv = kv->num_kv_heads;
+  p.Hq = Hq;
+  p.G = Hq / kv->num_kv_heads;
+  p.nq = nq;
+  p.R = pl.R;
+  p.n_rb = pl.n_rb;
+  p.nW = pl.nW;
+  p.min_share = pl.min_share;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.counters = static_cast<uint32_t*>(ws);
+  p.part = pl.record_bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + pl.counter_bytes) : nullptr;
+  p.part_bytes = (uint32_t)pl.record_bytes;
+  return launched(bd::launch_qattn(p, pl, kv->bits, stream));
+}
+}  // namespace
+
+bd_status bd_cache_append_q(const bd_qkv_desc* kv, const uint16_t* k_new, const uint16_t* v_new, int32_t n,
+                            const int32_t* counts, int32_t* idx, int32_t ld_idx, int32_t* nsel, hipStream_t stream) {
+  const bd_status st = check_qkv(kv, true, true, kv ? kv->num_kv_heads : 0);
+  if (st != BD_OK) return st;
+  if (n < 0) return fail(BD_ERR_INVALID_ARG, "n < 0");
+  if ((idx == nullptr) != (nsel == nullptr)) return fail(BD_ERR_INVALID_ARG, "idx and nsel go together");
+  if (idx && ld_idx < 0) return fail(BD_ERR_INVALID_ARG, "ld_idx < 0");
+  if (n == 0) return BD_OK;
+  if (!k_new || !v_new || !aligned(k_new, 16) || !aligned(v_new, 16))
+    return fail(BD_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned device pointers");
+  if (n > (1 << 30) || kv->num_seqs >= (1 << 22)) return fail(BD_ERR_UNSUPPORTED, "more than 2^30 rows or 2^22 - 1 sequences");
+  bd::QAppendParams p{};
+  p.kv = make_qview(*kv);
+  p.k_new = k_new;
+  p.v_new = v_new;
+  p.n = n;
+  p.counts = counts;
+  p.idx = idx;
+  p.nsel = nsel;
+  p.ld_idx = idx ? ld_idx : 0;
+  return launched(bd::launch_append_q(p, kv->bits, stream));
+}
+
+bd_status bd_cache_read_q(const bd_qkv_desc* kv, const int32_t* first, int32_t n, uint16_t* k_out, uint16_t* v_out,
+                          int64_t out_stride_seq, int64_t out_stride_head, int64_t out_stride_tok, hipStream_t stream) {
+  const bd_status st = check_qkv(kv, k_out != nullptr, v_out != nullptr, kv ? kv->num_kv_heads : 0);
+  if (st != BD_OK) return st;
+  if (n < 0) return fail(BD_ERR_INVALID_ARG, "n < 0");
+  if (!k_out && !v_out) return fail(BD_ERR_INVALID_ARG, "k_out and v_out are both NULL");
+  if (!aligned(k_out, 16) || !aligned(v_out, 16)) return fail(BD_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  if (out_stride_seq < 0 || out_stride_head < 0 || out_stride_tok < 0 || out_stride_seq % 8 || out_stride_head % 8 ||
+      out_stride_tok % 8)
+    return fail(BD_ERR_INVALID_ARG, "output strides must be non-negative multiples of 8 elements");
+  if (n > (1 << 30)) return fail(BD_ERR_UNSUPPORTED, "more than 2^30 rows");
+  if (n == 0) return BD_OK;
+  bd::QReadParams p{};
+  p.kv = make_qview(*kv);
+  p.first = first;
+  p.n = n;
+  p.k_out = k_out;
+  p.v_out = v_out;
+  p.stride_seq = out_stride_seq;
+  p.stride_head = out_stride_head;
+  p.stride_tok = out_stride_tok;
+  return launched(bd::launch_read_q(p, kv->bits, stream));
+}
+
+size_t bd_sparse_decode_attn_q_workspace_bytes(int32_t num_seqs, int32_t num_kv_heads, int32_t num_q_heads,
+                                               int32_t ld_idx) {
+  if (!shape_ok(num_seqs, num_kv_heads, num_q_heads) || ld_idx < 0) return 0;
+  const bd::QAttnPlan pl = bd::plan_qattn(num_seqs, num_kv_heads, num_q_heads, 1, ld_idx, true, false, 0);
+  return pl.nblk < 0 ? 0 : pl.ws_bytes;
+}
+
+bd_status bd_sparse_decode_attn_q(const bd_qkv_desc* kv, const uint16_t* q, int32_t num_q_heads, const int32_t* idx,
+                                  int32_t ld_idx, const int32_t* nsel, float scale, uint16_t* out, float* lse_out,
+                                  void* ws, size_t ws_bytes, hipStream_t stream) {
+  const bd_status st = check_qkv(kv, true, true, num_q_heads);
+  if (st != BD_OK) return st;
+  if (!q || !aligned(q, 16) || !out || !aligned(out, 16))
+    return fail(BD_ERR_INVALID_ARG, "q and out must be non-NULL and 16-byte aligned");
+  if (ld_idx < 0 || (ld_idx > 0 && !idx)) return fail(BD_ERR_INVALID_ARG, "idx / nsel / ld_idx invalid");
+  if (!nsel) return fail(BD_ERR_INVALID_ARG, "nsel is NULL");
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(BD_ERR_INVALID_ARG, "scale must be positive and finite");
+  return run_qattn(kv, q, num_q_heads, 1, idx, ld_idx, nsel, true, scale, out, lse_out, ws, ws_bytes, stream);
+}
+
+size_t bd_verify_attn_q_workspace_bytes(int32_t num_seqs, int32_t num_kv_heads, int32_t num_q_heads, int32_t gamma,
+                                        int32_t max_seq_len) {
+  if (!shape_ok(num_seqs, num_kv_heads, num_q_heads) || gamma < 0 || gamma > 4095 || max_seq_len < 0) return 0;
+  // the same for every layout
+  const bd::QAttnPlan pl = bd::plan_qattn(num_seqs, num_kv_heads, num_q_heads, gamma + 1, max_seq_len, false, false, 0);
+  return pl.nblk < 0 ? 0 : pl.ws_bytes;
+}
+
+bd_status bd_verify_attn_q(const bd_qkv_desc* kv, const uint16_t* q, int32_t num_q_heads, int32_t gamma, float scale,
+                           uint16_t* out, float* lse_out, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const bd_status st = check_qkv(kv, true, true, num_q_heads);
+  if (st != BD_OK) return st;
+  if (gamma < 0 || gamma > 4095) return fail(BD_ERR_INVALID_ARG, "gamma %d outside [0, 4095]", gamma);
+  if (!q || !aligned(q, 16) || !out || !aligned(out, 16))
+    return fail(BD_ERR_INVALID_ARG, "q and out must be non-NULL and 16-byte aligned");
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(BD_ERR_INVALID_ARG, "scale must be positive and finite");
+  return run_qattn(kv, q, num_q_heads, gamma + 1, nullptr, 0, nullptr, false, scale, out, lse_out, ws, ws_bytes, stream);
 }
 
 }  // extern "C"
