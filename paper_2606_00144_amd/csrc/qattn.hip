@@ -35,12 +35,10 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kTile = 32;                      // keys per wave step
-constexpr int kTab = 2048;                     // table entries (rows, or pages)
-constexpr int kGroup = 8;                      // records merged by one batch of loads
+constexpr int kGroup = 8;                      // records merged by one workgroup at a time
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                  // lazy-rescale headroom, log2 units
 constexpr uint32_t kAbsent = 0xFFFFFFFFu;
-constexpr int kMaxBlocks = 512;                // workgroups of a launch: two per CU
 
 // A tile in LDS: K's codes, V's codes, then the 32 scale words of K and of V.
 template <int BITS>
@@ -49,8 +47,6 @@ struct Tile {
   static constexpr int kParts = kRow / 64;               // 1 KiB loads per 16 rows of K or V
   static constexpr int kLoads = 4 * kParts + 1;          // loads of a tile
   static constexpr int kV = kTile * kRow, kS = 2 * kV, kBytes = kS + 2 * kTile * kBlocks;
-  static constexpr int kRing = BITS == 4 ? 4 : 2;
-
   // Load (h, e) of K brings rows of sub-tile h whole: lane l's 16 bytes land at 1024*(kParts*h + e) + 16*l, in row
   // slot l/4 (4 bits; 8e + l/8 with 8).  K's row r takes slot r, its chunk c position c ^ swizzle, so that 16 lanes
   // reading the same chunk of 16 rows meet no bank twice.  V's row 4a + b takes slot 4b + a, so that the 64 lanes
@@ -67,29 +63,45 @@ struct Tile {
   }
 };
 
-template <int BITS, int NT>
+// Workgroups that share a CU (and with them the waves of a SIMD), and the entries of a workgroup's table.
+constexpr int kRing = 2;                       // tile slots of a wave
+constexpr int kMaxBlocks = 512;                // workgroups of a launch
+template <int BITS, int NT, int ROWS>
+struct Config {
+  static constexpr int kPerCu = BITS == 8 || NT == 2 ? 2 : 3;
+  static constexpr int kTab = ROWS == kQContiguous ? 4 : ROWS == kQPages ? (BITS == 4 && NT == 1 ? 384 : 448) : BITS == 8 ? 1024 : 2048;
+};
+
+template <int BITS, int NT, int ROWS>
 struct Smem {
-  alignas(16) uint32_t tab[kTab];
+  alignas(16) uint32_t tab[Config<BITS, NT, ROWS>::kTab];
   union {
-    alignas(64) uint8_t ring[kWaves][Tile<BITS>::kRing][Tile<BITS>::kBytes];
-    struct {
-      alignas(16) float o[kWaves][16 * NT][kD + 4];
-      float m[kWaves][16 * NT], l[kWaves][16 * NT], lx[kWaves][16 * NT];
-    } merge;
+    alignas(64) uint8_t ring[kWaves][kRing][Tile<BITS>::kBytes];
+    float o[kWaves][16 * NT][kD / 2 + 4];      // half of the head dimension: the waves' states, when they merge
   } u;
+  union {
+    alignas(64) uint8_t q[16 * NT][kD * 2];    // query rows, chunk c (16 bytes) of row r at position c ^ k_swizzle(r % 16)
+    struct { float m[kWaves][16 * NT], l[kWaves][16 * NT], lx[kWaves][16 * NT]; } stat;
+  } r;
+  int32_t rowpos[16 * NT];    // position of each query row (INT_MAX: sees every key)
+  int32_t nan_from[kBlocks];  // first position whose V holds not-a-numbers in block b (INT_MAX: none)
   int32_t last;
+  int32_t first_hole;         // first tile of the table with an absent key
 };
 
 template <int NT>
 struct RowState {
   f32x4 o[NT][8];     // O^T[d-tile][row tile]: register i of d-tile dt holds d = 32*(l/16) + 8*i + dt
-  f32x4 l[NT];        // sums of the rounded weights (every register holds the row's)
   float m[NT];        // reference maximum (log2 domain)
-  float lx[NT];       // this lane's sum of the unrounded weights (log-sum-exp only)
+  float l[NT];        // this lane's sum of the rounded weights
+  float lx[NT];       // and of the unrounded ones (log-sum-exp only)
 };
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 __device__ inline f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
-__device__ inline uint32_t as_word(const __attribute__((ext_vector_type(2))) __bf16& v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ inline uint32_t as_word(const bf16x2& v) { return __builtin_bit_cast(uint32_t, v); }
 
 // 8 values of a row as bf16 from their codes (c: one word with 4 bits, two with 8) and the scale's exponent bits.
 template <int BITS>
@@ -135,59 +147,76 @@ __device__ inline void read_tile(TileRegs<BITS>& T, const uint8_t* t, int lane) 
   }
 }
 
-// One tile of one wave.  `dirty` (uniform): some key of the tile is absent or hidden from some row; key slot i of
-// this lane is absent unless bit i of `there`, and lies at position pos0 + 16*(i/4) + i%4.
-template <int BITS, int NT>
-__device__ inline void tile_step(RowState<NT>& st, TileRegs<BITS>& T, const bf16x8 (&qop)[NT][4], const int (&rowpos)[NT],
-                                 float scale_log2, bool dirty, uint32_t there, int pos0, bool want_lx) {
+// One tile of one wave.  DIRTY: some key of the tile is absent or hidden from some row; key slot i of this lane is
+// absent unless bit i of `there`, and lies at position pos0 + 16*(i/4) + i%4.
+template <int BITS, int NT, bool DIRTY, bool LSE>
+__device__ inline void tile_step(RowState<NT>& st, TileRegs<BITS>& T, const uint8_t (*q)[kD * 2], float scale_log2,
+                                 uint32_t there, int pos0, int lane, const int32_t* rowpos, int32_t* nan_from) {
+  if constexpr (DIRTY) {
+    // What lies in absent rows (stale memory) must not reach the product: 0 * NaN.  Nor may a block that is not a
+    // number reach rows that do not see its key: it is taken out, and the first position of such blocks is kept,
+    // from which on the rows' outputs become not a number when the waves merge.
+    int first = 0x7FFFFFFF;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool present = (there >> i) & 1u, bad = (T.vs[i] & 0x7F800000u) == 0x7F800000u;
+      if (present && bad && pos0 + 16 * (i >> 2) + (i & 3) < first) first = pos0 + 16 * (i >> 2) + (i & 3);
+#pragma unroll
+      for (int e = 0; e < Tile<BITS>::kParts; ++e) T.v[i][e] = present && !bad ? T.v[i][e] : 0u;
+      T.vs[i] = present && !bad ? T.vs[i] : 0x3F800000u;
+    }
+    if (first != 0x7FFFFFFF) atomicMin(&nan_from[(lane & 15) >> 2], first);
+  }
+  const int lg = lane >> 4, lr = lane & 15;
   f32x4 sc[2][NT];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    bf16x8 kop[4];
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if constexpr (BITS == 4) kop[j] = as_bf16x8(to_bf16<4>(T.k[h][0][j], 0u, T.ks[h]));
-      else kop[j] = as_bf16x8(to_bf16<8>(T.k[h][j >> 1][2 * (j & 1)], T.k[h][j >> 1][2 * (j & 1) + 1], T.ks[h]));
+    for (int nt = 0; nt < NT; ++nt) sc[h][nt] = zero4();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    bf16x8 kop[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if constexpr (BITS == 4) kop[h] = as_bf16x8(to_bf16<4>(T.k[h][0][j], 0u, T.ks[h]));
+      else kop[h] = as_bf16x8(to_bf16<8>(T.k[h][j >> 1][2 * (j & 1)], T.k[h][j >> 1][2 * (j & 1) + 1], T.ks[h]));
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      f32x4 a = zero4();
+      const bf16x8 qop = *reinterpret_cast<const bf16x8*>(&q[16 * nt + lr][16 * ((4 * lg + j) ^ k_swizzle(lr))]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[j], qop[nt][j], a, 0, 0, 0);
-      sc[h][nt] = a;
+      for (int h = 0; h < 2; ++h) sc[h][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[h], qop, sc[h][nt], 0, 0, 0);
     }
   }
-  if (dirty) {
+  if constexpr (DIRTY) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool present = (there >> i) & 1u;
-      const int pos = pos0 + 16 * (i >> 2) + (i & 3);
+    for (int nt = 0; nt < NT; ++nt) {
+      const int last = rowpos[16 * nt + lr];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-        if (!(present && pos <= rowpos[nt])) sc[i >> 2][nt][i & 3] = -INFINITY;
-      // what lies in absent rows (stale memory) must not reach the products: 0 * NaN
-#pragma unroll
-      for (int e = 0; e < Tile<BITS>::kParts; ++e) T.v[i][e] = present ? T.v[i][e] : 0u;
-      T.vs[i] = present ? T.vs[i] : 0x3F800000u;
+      for (int i = 0; i < 8; ++i)
+        if (!(((there >> i) & 1u) && pos0 + 16 * (i >> 2) + (i & 3) <= last)) sc[i >> 2][nt][i & 3] = -INFINITY;
     }
   }
 
+  // The reference maximum is raised when a score exceeds it by more than kSlack: the lanes look at their own scores,
+  // and only then at each other's.
   float mx[NT];
   bool raise = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    float v = -INFINITY;
+    float x = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v = fmaxf(v, sc[i >> 2][nt][i & 3]);
-    mx[nt] = max_xor32(max_xor16(v)) * scale_log2;    // scale > 0: the max commutes with it
+    for (int i = 0; i < 8; ++i) x = fmaxf(x, sc[i >> 2][nt][i & 3]);
+    mx[nt] = x * scale_log2;                          // scale > 0: the max commutes with it
     raise |= mx[nt] > st.m[nt] + kSlack;
   }
   if (__builtin_expect(__builtin_amdgcn_ballot_w64(raise) != 0, 0)) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const bool up = mx[nt] > st.m[nt] + kSlack;
-      const float alpha = up ? __builtin_amdgcn_exp2f(st.m[nt] - mx[nt]) : 1.f;   // 0 on the first visible tile
-      st.m[nt] = up ? mx[nt] : st.m[nt];
+      const float x = max_xor32(max_xor16(mx[nt]));
+      const bool up = x > st.m[nt] + kSlack;
+      const float alpha = up ? __builtin_amdgcn_exp2f(st.m[nt] - x) : 1.f;   // 0 on the first visible tile
+      st.m[nt] = up ? x : st.m[nt];
       st.l[nt] *= alpha;
       st.lx[nt] *= alpha;
 #pragma unroll
@@ -195,7 +224,7 @@ __device__ inline void tile_step(RowState<NT>& st, TileRegs<BITS>& T, const bf16
     }
   }
 
-  const bf16x8 ones = as_bf16x8(u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+  const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
   bf16x8 pop[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -203,58 +232,26 @@ __device__ inline void tile_step(RowState<NT>& st, TileRegs<BITS>& T, const bf16
     float pv[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) pv[i] = __builtin_amdgcn_exp2f(fmaf(sc[i >> 2][nt][i & 3], scale_log2, -muse));
-    u32x4 pw;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) pw[i] = pack_bf16x2(pv[2 * i], pv[2 * i + 1]);
-    pop[nt] = as_bf16x8(pw);
-    if (want_lx) {
+    if constexpr (LSE) {
       float sx = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) sx += pv[i];
       st.lx[nt] += sx;
     }
-    st.l[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pop[nt], st.l[nt], 0, 0, 0);
+    u32x4 pw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w = pack_bf16x2(pv[2 * i], pv[2 * i + 1]);
+      // hidden from the compiler, which took the first pair of the operand below for all four
+      asm("" : "+v"(w));
+      st.l[nt] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), ones, st.l[nt], false);
+      pw[i] = w;
+    }
+    pop[nt] = as_bf16x8(pw);
   }
-
   u32x4 v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = to_bf16<BITS>(T.v[i][0], T.v[i][Tile<BITS>::kParts - 1], T.vs[i]);
-
-  // A value that is not a number belongs only to the rows that see its key: 0 * NaN in the product would reach the
-  // others.  Such values are taken out of the product and counted, per row and d, by one of ones.
-  if (dirty) {
-    uint32_t bad = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-        bad |= ((v[i][w] & 0x7F80u) == 0x7F80u || (v[i][w] & 0x7F800000u) == 0x7F800000u) ? 1u : 0u;
-    if (__builtin_amdgcn_ballot_w64(bad != 0u) != 0) {
-      u32x4 ind[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const bool lo = (v[i][w] & 0x7F80u) == 0x7F80u, hi = (v[i][w] & 0x7F800000u) == 0x7F800000u;
-          ind[i][w] = (lo ? 0x3F80u : 0u) | (hi ? 0x3F800000u : 0u);
-          v[i][w] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-        }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        u32x4 sees = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (((there >> i) & 1u) && pos0 + 16 * (i >> 2) + (i & 3) <= rowpos[nt]) sees[i >> 1] |= (i & 1) ? 0x3F800000u : 0x3F80u;
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-          const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt_operand(ind, dt), as_bf16x8(sees), zero4(), 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (n[i] > 0.f) st.o[nt][dt][i] = __uint_as_float(0x7FC00000u);
-        }
-      }
-    }
-  }
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt) {
     const bf16x8 vt = vt_operand(v, dt);
@@ -264,14 +261,11 @@ __device__ inline void tile_step(RowState<NT>& st, TileRegs<BITS>& T, const bf16
   }
 }
 
-// Wait until at most `tiles` tiles of this wave are still on their way.
-template <int BITS>
-__device__ inline void wait_tiles(int tiles) {
-  constexpr int n = Tile<BITS>::kLoads;
-  if (tiles >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * n) : "memory");
-  else if (tiles == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * n) : "memory");
-  else if (tiles == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
-  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+// The same value, of which the compiler knows nothing: what is computed from it is computed where it stands, not kept
+// in registers over the loops around (or before) it.
+__device__ inline int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // Keys of sequence s's units, and its length.
@@ -284,25 +278,45 @@ __device__ inline int unit_keys(const QAttnParams& p, int s, int& L) {
 // Tiles of a unit: an empty one still takes part, its outputs have to be written.
 __device__ inline int unit_tiles(int n) { return n > 0 ? (int)(((int64_t)n + kTile - 1) / kTile) : 1; }
 
-__device__ inline int wave_scan(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+// Inclusive sums over the lanes.
+template <int CTRL, int ROWMASK>
+__device__ inline int add_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWMASK, 0xF, false); }
+__device__ inline int wave_scan(int x) {
+  x = add_dpp<0x111, 0xF>(x);    // row_shr 1, 2, 4, 8: within 16 lanes
+  x = add_dpp<0x112, 0xF>(x);
+  x = add_dpp<0x114, 0xF>(x);
+  x = add_dpp<0x118, 0xF>(x);
+  x = add_dpp<0x142, 0xA>(x);    // the last lane of a row of 16 to the next row (rows 1 and 3)
+  return add_dpp<0x143, 0xC>(x); // lane 31 to rows 2 and 3
 }
 
-template <int BITS, int NT, int ROWS>
-__global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
+// Every kernel argument requested at entry, so that they cost one round trip to the memory that holds them rather
+// than one per line where first used (attn.hip's fetch_args says more); returns 0.  Left to the compiler, the lines
+// past the first came one after the other, XCD after XCD: a workgroup began its loads 2 to 15 us after its start
+// (8 heads of one 8K sequence, 26.7 us).
+__device__ inline int fetch_args(const QAttnParams& p) {
+  int z0, z1, z2;
+  asm("s_mov_b32 %0, 0" : "=s"(z0) : "s"(p.kv.k), "s"(p.kv.v), "s"(p.kv.k_scale), "s"(p.kv.v_scale), "s"(p.kv.seq_lens),
+      "s"(p.kv.page_table), "s"(p.kv.stride_seq), "s"(p.kv.stride_head), "s"(p.kv.stride_tok));
+  asm("s_mov_b32 %0, 0" : "=s"(z1) : "s"(z0), "s"(p.kv.stride_page), "s"(p.kv.max_seq_len), "s"(p.kv.page_size),
+      "s"(p.kv.max_pages_per_seq), "s"(p.kv.num_pages), "s"(p.q), "s"(p.out), "s"(p.lse), "s"(p.idx), "s"(p.nsel));
+  asm("s_mov_b32 %0, 0" : "=s"(z2) : "s"(z1), "s"(p.ld_idx), "s"(p.S), "s"(p.Hkv), "s"(p.Hq), "s"(p.G), "s"(p.nq),
+      "s"(p.R), "s"(p.n_rb), "s"(p.nW), "s"(p.min_share), "s"(p.scale_log2), "s"(p.part), "s"(p.part_bytes),
+      "s"(p.counters));
+  return z2;
+}
+
+template <int BITS, int NT, int ROWS, bool LSE>
+__global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qattn_kernel(QAttnParams p) {
   using TL = Tile<BITS>;
+  constexpr int kTab = Config<BITS, NT, ROWS>::kTab;
   constexpr int kRows = 16 * NT;
   constexpr int kRec = kRows * (4 + kD);       // floats of a record: (m, l, lx, -) per row, then the outputs
-  __shared__ Smem<BITS, NT> sm;
+  __shared__ Smem<BITS, NT, ROWS> sm;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lg = lane >> 4, lr = lane & 15;
-  const int bid = xcd_remap(blockIdx.x, gridDim.x);
+  const int bid = xcd_remap(blockIdx.x + fetch_args(p), gridDim.x);
   const int share = bid / p.n_rb, rb = bid - share * p.n_rb;
   const bool gather = p.idx != nullptr;
 
@@ -311,7 +325,7 @@ __global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
   for (int s0 = 0; s0 < p.S; s0 += kWave) {
     int L = 0, w = 0;
     if (s0 + lane < p.S) w = unit_tiles(unit_keys(p, s0 + lane, L)) * p.Hkv;
-    w = wave_scan(w, lane);
+    w = wave_scan(w);
     if (s0 == 0) first_w = w;
     total += __builtin_amdgcn_readlane(w, kWave - 1);
   }
@@ -328,7 +342,7 @@ __global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
       int L = 0;
       w = 0;
       if (s0 + lane < p.S) w = unit_tiles(unit_keys(p, s0 + lane, L)) * p.Hkv;
-      w = wave_scan(w, lane);
+      w = wave_scan(w);
     }
     const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(acc + w <= pos));
     if (c < kWave) {
@@ -341,69 +355,82 @@ __global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
   s = __builtin_amdgcn_readfirstlane(s);
   before = __builtin_amdgcn_readfirstlane(before);
 
-  int L, n = unit_keys(p, s, L);
+  int L, n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
+  L = __builtin_amdgcn_readfirstlane(L);
   int T = unit_tiles(n);
   int g = (pos - before) / T;
   int unit0 = before + g * T;                  // the unit's first tile in the stream
 
   const uint32_t ring_lds = lds_addr(&sm.u.ring[wave][0][0]);
   const uint32_t tok = (uint32_t)p.kv.stride_tok, tok_bytes = tok * (uint32_t)TL::kRow;   // 15 rows below 2^31: host-checked
-  const uint8_t* const scales = lane < kTile ? p.kv.k_scale : p.kv.v_scale;
-  const bool want_lx = p.lse != nullptr;
+  uint32_t k_off[TL::kParts], v_off[TL::kParts];           // this lane's bytes of a whole sub-tile's loads
+#pragma unroll
+  for (int e = 0; e < TL::kParts; ++e) {
+    k_off[e] = (uint32_t)TL::k_row(lane, e) * tok_bytes + 16u * (uint32_t)TL::k_chunk(lane, e);
+    v_off[e] = (uint32_t)TL::v_row(lane, e) * tok_bytes + 16u * (uint32_t)TL::v_chunk(lane);
+  }
 
   for (;;) {   // ---- one piece: tiles [t0, t1) of unit (s, g)
     const int t0 = pos - unit0;
     const int t1 = T - t0 < end - pos ? T : t0 + (end - pos);
     const int tn = (n + kTile - 1) / kTile < t1 ? (n + kTile - 1) / kTile : t1;   // tiles that hold keys
 
-    bf16x8 qop[NT][4];
-    int rowpos[NT];
+    const int lane_q = here(lane), lgq = lane_q >> 4, lrq = lane_q & 15;
     RowState<NT> st;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int r = rb * kRows + 16 * nt + lr;
-      const bool valid = r < p.R;
-      const int j = valid ? r / p.G : 0;
-      const int h = g * p.G + (valid ? r - j * p.G : 0);
-      // selected entries lie below the length, and the one query at its end sees them all
-      rowpos[nt] = valid && !gather ? L - p.nq + j : 0x7FFFFFFF;
-      const uint16_t* qrow = p.q + (((int64_t)s * p.nq + j) * p.Hq + h) * kD + 32 * lg;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) qop[nt][k] = as_bf16x8(valid ? load16(qrow + 8 * k) : u32x4{0u, 0u, 0u, 0u});
       st.m[nt] = -INFINITY;
-      st.l[nt] = zero4();
-      st.lx[nt] = 0.f;
+      st.l[nt] = st.lx[nt] = 0.f;
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) st.o[nt][dt] = zero4();
     }
+    // each row's position: selected entries lie below the length, and the one query at its end sees them all
+    if (lane_q < 4 * NT) {
+      const int r = 4 * NT * wave + lane_q, row = rb * kRows + r;
+      sm.rowpos[r] = row < p.R && !gather ? L - p.nq + row / p.G : 0x7FFFFFFF;
+    }
+    // query rows to LDS, four a load; rows past the last one repeat it
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+      const int r0 = 4 * (NT * wave + k), r = r0 + lgq;
+      const int row = rb * kRows + r < p.R ? rb * kRows + r : p.R - 1;
+      const int j = row / p.G;
+      dma16_hidden(p.q + (((int64_t)s * p.nq + j) * p.Hq + g * p.G + (row - j * p.G)) * kD + 8 * (lrq ^ k_swizzle(r & 15)),
+                   lds_addr(&sm.r.q[r0][0]));
+    }
+    if (tid < kBlocks) sm.nan_from[tid] = 0x7FFFFFFF;
     const int minpos = gather ? 0x7FFFFFFF : L - p.nq + rb * kRows / p.G;         // position of the block's first row
-    const int64_t head_row = (int64_t)s * p.kv.stride_seq + (int64_t)g * p.kv.stride_head;
+    const uint32_t head_row = (uint32_t)((int64_t)s * p.kv.stride_seq + (int64_t)g * p.kv.stride_head);
 
     for (int c0 = t0; c0 < tn;) {   // ---- as many tiles as the table covers
       int c1 = tn;
-      int page0 = 0, psub = 1;
-      float inv_psub = 1.f;
-      bool holes = false;            // some key that the table covers is absent
+      // tiles from first_dirty on may hold keys that are absent or hidden from some row
+      int first_dirty = n / kTile;
+      if (!gather && (minpos + 1) / kTile < first_dirty) first_dirty = minpos < 0 ? 0 : (minpos + 1) / kTile;
+      bool holes = false;            // some page that the table covers is outside the pool
       if constexpr (ROWS == kQPages) {
-        psub = p.kv.page_size >> 4;
-        inv_psub = __builtin_amdgcn_rcpf((float)psub);
-        const int64_t most = (int64_t)(kTab - 2) * psub / 2;
-        if (c1 - c0 > most) c1 = c0 + (int)most;
-        page0 = div_small(2 * c0, psub, inv_psub);
-        const int last = (c1 * kTile < n ? c1 * kTile : n) - 1;
-        const int np = div_small(last >> 4, psub, inv_psub) - page0 + 1;
-        const int32_t* prow = p.kv.page_table + (int64_t)s * p.kv.max_pages_per_seq + page0;
+        // one entry per sub-tile: the row of its first key
+        if (c1 - c0 > kTab / 2) c1 = c0 + kTab / 2;
+        const int32_t* prow = p.kv.page_table + (int64_t)s * p.kv.max_pages_per_seq;
         int bad = 0;
-        for (int j = tid; j < np; j += kThreads) {
-          const int pg = prow[j];
-          const bool ok = (unsigned)pg < (unsigned)p.kv.num_pages;
-          bad |= ok ? 0 : 1;
-          sm.tab[j] = ok ? (uint32_t)((int64_t)pg * p.kv.stride_page + (int64_t)g * p.kv.stride_head) : kAbsent;
+        for (int j = tid; j < 2 * (c1 - c0); j += kThreads) {
+          const int t = c0 * kTile + 16 * j;
+          uint32_t x = kAbsent;
+          if (t < n) {
+            const int pi = t / p.kv.page_size, pg = prow[pi];
+            if ((unsigned)pg < (unsigned)p.kv.num_pages)
+              x = (uint32_t)((int64_t)pg * p.kv.stride_page + (int64_t)g * p.kv.stride_head + (int64_t)(t - pi * p.kv.page_size) * tok);
+            else bad = 1;
+          }
+          sm.tab[j] = x;
         }
-        holes = __syncthreads_or(bad) != 0;
+        holes = __builtin_amdgcn_readfirstlane(__syncthreads_or(bad)) != 0;
+        if (holes) first_dirty = c0;
       } else if constexpr (ROWS == kQTable) {
         if (c1 - c0 > kTab / kTile) c1 = c0 + kTab / kTile;
         const int32_t* list = gather ? p.idx + ((int64_t)s * p.Hkv + g) * p.ld_idx : nullptr;
+        if (tid == 0) sm.first_hole = 0x7FFFFFFF;
+        __syncthreads();
         for (int i = tid; i < (c1 - c0) * kTile; i += kThreads) {
           const int e = c0 * kTile + i;
           int t = -1;
@@ -414,26 +441,32 @@ __global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
             if (row >= 0) row += (int64_t)g * p.kv.stride_head;
           }
           sm.tab[i] = row >= 0 ? (uint32_t)row : kAbsent;
+          if (row < 0) atomicMin(&sm.first_hole, c0 + i / kTile);
         }
         __syncthreads();
+        const int hole = __builtin_amdgcn_readfirstlane(sm.first_hole);
+        if (hole < first_dirty) first_dirty = hole;
       }
 
-      // row of a sub-tile's first key (uniform); `lim`: the last row of it that may be read (contiguous)
-      auto sub_row = [&](int t, int& lim) -> int64_t {
-        lim = 15;
-        if constexpr (ROWS == kQContiguous) {
-          if (t + 15 < n) return head_row + (int64_t)t * tok;
-          lim = t < n ? n - 1 - t : 0;
-          return head_row + (int64_t)(t < n ? t : n - 1) * tok;
-        } else {
-          if (t >= n) return 0;
-          const int pi = div_small(t >> 4, psub, inv_psub);
-          const uint32_t b = (uint32_t)__builtin_amdgcn_readfirstlane((int)sm.tab[pi - page0]);
-          return b == kAbsent ? 0 : (int64_t)b + (int64_t)(t - pi * p.kv.page_size) * tok;
+      // rows of a tile's sub-tiles, their first keys' (uniform), and the last row of each that may be read
+      struct Where { uint32_t row[2]; int lim[2]; };
+      auto where = [&](int c) {
+        Where at{{0u, 0u}, {15, 15}};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int t = c * kTile + 16 * h;
+          if constexpr (ROWS == kQContiguous) {
+            if (t + 15 >= n) at.lim[h] = t < n ? n - 1 - t : 0;
+            at.row[h] = head_row + (uint32_t)(t < n ? t : n - 1) * tok;
+          } else if constexpr (ROWS == kQPages) {
+            const uint32_t x = (uint32_t)__builtin_amdgcn_readfirstlane((int)sm.tab[2 * (c - c0) + h]);
+            at.row[h] = x == kAbsent ? 0u : x;             // past the keys, or absent: any row
+          }
         }
+        return at;
       };
       // direct loads of tile c into ring slot `slot`
-      auto issue = [&](int c, int slot) {
+      auto issue = [&](int c, int slot, const Where& at) {
         const uint32_t dst = ring_lds + (uint32_t)(slot * TL::kBytes);
         if constexpr (ROWS == kQTable) {
           const uint32_t* tab = sm.tab + (c - c0) * kTile;
@@ -442,129 +475,185 @@ __global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < TL::kParts; ++e) {
-              const uint32_t at = dst + 1024u * (uint32_t)(TL::kParts * h + e);
+              const uint32_t to = dst + 1024u * (uint32_t)(TL::kParts * h + e);
               const uint8_t* kp = p.kv.k + (uint64_t)row_at(16 * h + TL::k_row(lane, e)) * TL::kRow + 16 * TL::k_chunk(lane, e);
               const uint8_t* vp = p.kv.v + (uint64_t)row_at(16 * h + TL::v_row(lane, e)) * TL::kRow + 16 * TL::v_chunk(lane);
-              dma16_hidden(reinterpret_cast<const uint16_t*>(kp), at);
-              dma16_hidden(reinterpret_cast<const uint16_t*>(vp), at + TL::kV);
+              dma16_hidden(reinterpret_cast<const uint16_t*>(kp), to);
+              dma16_hidden(reinterpret_cast<const uint16_t*>(vp), to + TL::kV);
             }
-          dma4_hidden(scales + (uint64_t)row_at(lane & 31) * kBlocks, dst + TL::kS);
+          dma4_hidden((lane < kTile ? p.kv.k_scale : p.kv.v_scale) + (uint64_t)row_at(lane & 31) * kBlocks, dst + TL::kS);
         } else {
-          int lim[2];
-          const int64_t r0 = sub_row(c * kTile, lim[0]), r1 = sub_row(c * kTile + 16, lim[1]);
-          const int64_t row[2] = {r0, r1};
+          const uint32_t row0 = at.row[0], row1 = at.row[1];
+          const int lim0 = at.lim[0], lim1 = at.lim[1];
+          auto loads = [&](auto whole_tag) {
+            constexpr bool WHOLE = decltype(whole_tag)::value;
+            const int lane_i = WHOLE ? lane : here(lane);
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+              const uint8_t* kb = p.kv.k + (uint64_t)(h ? row1 : row0) * TL::kRow;
+              const uint8_t* vb = p.kv.v + (uint64_t)(h ? row1 : row0) * TL::kRow;
 #pragma unroll
-            for (int e = 0; e < TL::kParts; ++e) {
-              const uint32_t at = dst + 1024u * (uint32_t)(TL::kParts * h + e);
-              const int kr = TL::k_row(lane, e) < lim[h] ? TL::k_row(lane, e) : lim[h];
-              const int vr = TL::v_row(lane, e) < lim[h] ? TL::v_row(lane, e) : lim[h];
-              dma16_hidden(reinterpret_cast<const uint16_t*>(p.kv.k + row[h] * TL::kRow),
-                           (uint32_t)kr * tok_bytes + 16u * (uint32_t)TL::k_chunk(lane, e), at);
-              dma16_hidden(reinterpret_cast<const uint16_t*>(p.kv.v + row[h] * TL::kRow),
-                           (uint32_t)vr * tok_bytes + 16u * (uint32_t)TL::v_chunk(lane), at + TL::kV);
+              for (int e = 0; e < TL::kParts; ++e) {
+                const uint32_t to = dst + 1024u * (uint32_t)(TL::kParts * h + e);
+                uint32_t ko = k_off[e], vo = v_off[e];
+                if (!WHOLE) {
+                  const int lim = h ? lim1 : lim0;
+                  const int kr = TL::k_row(lane_i, e) < lim ? TL::k_row(lane_i, e) : lim;
+                  const int vr = TL::v_row(lane_i, e) < lim ? TL::v_row(lane_i, e) : lim;
+                  ko = (uint32_t)kr * tok_bytes + 16u * (uint32_t)TL::k_chunk(lane_i, e);
+                  vo = (uint32_t)vr * tok_bytes + 16u * (uint32_t)TL::v_chunk(lane_i);
+                }
+                dma16_hidden(reinterpret_cast<const uint16_t*>(kb), ko, to);
+                dma16_hidden(reinterpret_cast<const uint16_t*>(vb), vo, to + TL::kV);
+              }
             }
-          const int hs = (lane >> 4) & 1;
-          const int sr = lr < (hs ? lim[1] : lim[0]) ? lr : (hs ? lim[1] : lim[0]);
-          dma4_hidden(scales + (uint64_t)((hs ? r1 : r0) + (int64_t)sr * tok) * kBlocks, dst + TL::kS);
+            const int lane_s = here(lane);                 // three instructions a tile rather than three registers
+            const bool upper = (lane_s & 16) != 0;
+            int sr = lane_s & 15;
+            if (!WHOLE) sr = sr < (upper ? lim1 : lim0) ? sr : (upper ? lim1 : lim0);
+            const uint8_t* sb = lane_s < kTile ? p.kv.k_scale : p.kv.v_scale;
+            dma4_hidden(sb + (uint64_t)((upper ? row1 : row0) + (uint32_t)sr * tok) * kBlocks, dst + TL::kS);
+          };
+          if (ROWS == kQPages || c * kTile + kTile <= n) loads(BoolTag<true>{});
+          else loads(BoolTag<false>{});
         }
       };
 
       const int mine = c1 - c0 > wave ? (c1 - c0 - wave + kWaves - 1) / kWaves : 0;   // tiles of this wave
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // only tiles are counted from here on
-      for (int i = 0; i < TL::kRing && i < mine; ++i) issue(c0 + wave + i * kWaves, i);
-      for (int i = 0, slot = 0; i < mine; ++i, slot = slot + 1 == TL::kRing ? 0 : slot + 1) {
+      for (int i = 0; i < kRing && i < mine; ++i) issue(c0 + wave + i * kWaves, i, where(c0 + wave + i * kWaves));
+      if (c0 == t0) {
+        // the query rows, which were asked for first, and every load and store before them
+        if (mine >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * TL::kLoads) : "memory");
+        else if (mine == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TL::kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+      int i = 0, slot = 0;
+      // tile i of this wave: its codes to registers, its slot filled again, the products
+      auto step = [&](auto dirty_tag) {
+        constexpr bool DIRTY = decltype(dirty_tag)::value;
         const int c = c0 + wave + i * kWaves;
-        const int later = mine - 1 - i < TL::kRing - 1 ? mine - 1 - i : TL::kRing - 1;
-        wait_tiles<BITS>(later);
+        if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TL::kLoads) : "memory");   // the next tile is on its way
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const bool more = i + kRing < mine;
+        const Where next = where(more ? c + kRing * kWaves : c);
         TileRegs<BITS> tile;
         read_tile<BITS>(tile, sm.u.ring[wave][slot], lane);
-        // key slot 4h + i of this lane: key c*32 + 16h + 4*lg + i
+        // key slot 4h + j of this lane: key c*32 + 16h + 4*lg + j
         const int key0 = c * kTile + 4 * lg;
-        bool dirty = c * kTile + kTile > n || (!gather && c * kTile + kTile - 1 > minpos);
         uint32_t there = 0xFFu;
-        if constexpr (ROWS == kQTable) {
-          const uint64_t absent = __builtin_amdgcn_ballot_w64(sm.tab[(c - c0) * kTile + (lane & 31)] == kAbsent);
-          dirty = dirty || (uint32_t)absent != 0u;
-          const uint32_t ok = ~(uint32_t)absent >> (4 * lg);
-          there = (ok & 0xFu) | ((ok >> 12) & 0xF0u);
-        } else if (dirty || holes) {
-          there = 0u;
+        if constexpr (DIRTY) {
+          if constexpr (ROWS == kQTable) {
+            const uint32_t ok = ~(uint32_t)__builtin_amdgcn_ballot_w64(sm.tab[(c - c0) * kTile + (lane & 31)] == kAbsent) >> (4 * lg);
+            there = (ok & 0xFu) | ((ok >> 12) & 0xF0u);
+          } else {
+            there = 0u;
 #pragma unroll
-          for (int i2 = 0; i2 < 8; ++i2) there |= key0 + 16 * (i2 >> 2) + (i2 & 3) < n ? 1u << i2 : 0u;
-          if constexpr (ROWS == kQPages) {
-            if (holes) {
-              dirty = true;
+            for (int j = 0; j < 8; ++j) there |= key0 + 16 * (j >> 2) + (j & 3) < n ? 1u << j : 0u;
+            if constexpr (ROWS == kQPages) {
+              if (holes) {
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int t = c * kTile + 16 * h;
-                if (t < n && sm.tab[div_small(t >> 4, psub, inv_psub) - page0] == kAbsent) there &= h ? 0x0Fu : 0xF0u;
+                for (int h = 0; h < 2; ++h)
+                  if (sm.tab[2 * (c - c0) + h] == kAbsent) there &= h ? 0x0Fu : 0xF0u;
               }
             }
           }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read: it may be filled again
-        if (i + TL::kRing < mine) issue(c + TL::kRing * kWaves, slot);
-        tile_step<BITS, NT>(st, tile, qop, rowpos, p.scale_log2, dirty, there, key0, want_lx);
-      }
+        if (more) issue(c + kRing * kWaves, slot, next);
+        tile_step<BITS, NT, DIRTY, LSE>(st, tile, sm.r.q, p.scale_log2, there, key0, lane, sm.rowpos, sm.nan_from);
+        ++i;
+        slot ^= 1;
+      };
+      // in loops of their own: as two branches of one, the accumulators were copied at every tile
+      const int clean = first_dirty > c0 + wave ? (first_dirty - c0 - wave + kWaves - 1) / kWaves : 0;
+      while (i < mine && i < clean) step(BoolTag<false>{});
+      while (i < mine) step(BoolTag<true>{});
       c0 = c1;
       if (ROWS != kQContiguous && c0 < tn) __syncthreads();   // the table is filled again
     }
 
-    // ---- the four waves' states, through LDS
+    // ---- the four waves' states, through LDS, half of the head dimension at a time.  Thread -> row r and kPer
+    // outputs of each half: those at local .. of the half, which lie at d_at(half) ..
+    constexpr int kPer = kRows * kD / 2 / kThreads;        // 4 or 8
+    const int tid_m = here(tid), lgm = (tid_m >> 4) & 3, lrm = tid_m & 15;
+    const int r = tid_m / (kD / 2 / kPer), local = (tid_m % (kD / 2 / kPer)) * kPer;
+    auto d_at = [&](int half) { return 32 * (local >> 4) + 16 * half + (local & 15); };
+    float M = -INFINITY, Ls = 0.f, Lx = 0.f, acc[2][kPer];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the query rows of a piece without keys
     __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float lx = st.lx[nt];
-      lx += shfl_xor_f(lx, 16);
-      lx += shfl_xor_f(lx, 32);
-      const int r = 16 * nt + lr;
-      if (lg == 0) {
-        sm.u.merge.m[wave][r] = st.m[nt];
-        sm.u.merge.l[wave][r] = st.l[nt][0];
-        sm.u.merge.lx[wave][r] = lx;
+      float l = st.l[nt], lx = st.lx[nt];
+      l += shfl_xor_f(l, 16);
+      l += shfl_xor_f(l, 32);
+      if constexpr (LSE) {
+        lx += shfl_xor_f(lx, 16);
+        lx += shfl_xor_f(lx, 32);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float* dst = &sm.u.merge.o[wave][r][32 * lg + 8 * i];
-        *reinterpret_cast<f32x4*>(dst) = f32x4{st.o[nt][0][i], st.o[nt][1][i], st.o[nt][2][i], st.o[nt][3][i]};
-        *reinterpret_cast<f32x4*>(dst + 4) = f32x4{st.o[nt][4][i], st.o[nt][5][i], st.o[nt][6][i], st.o[nt][7][i]};
+      if (lgm == 0) {
+        sm.r.stat.m[wave][16 * nt + lrm] = st.m[nt];
+        sm.r.stat.l[wave][16 * nt + lrm] = l;
+        sm.r.stat.lx[wave][16 * nt + lrm] = lx;
       }
     }
-    __syncthreads();
-    constexpr int kPer = kRows * kD / kThreads;            // outputs per thread: 8 or 16
-    const int r = tid / (kD / kPer), d0 = (tid % (kD / kPer)) * kPer;
-    float M = -INFINITY, Ls = 0.f, Lx = 0.f, acc[kPer];
+    float wt[kWaves];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm.u.merge.m[w][r]);
-    const float Mu = M == -INFINITY ? 0.f : M;
+    for (int half = 0; half < 2; ++half) {
+      if (half == 1) __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) acc[e] = 0.f;
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float wt = exp2f(sm.u.merge.m[w][r] - Mu);
-      Ls += wt * sm.u.merge.l[w][r];
-      Lx += wt * sm.u.merge.lx[w][r];
+        for (int i = 2 * half; i < 2 * half + 2; ++i) {
+          float* dst = &sm.u.o[wave][16 * nt + lrm][16 * lgm + 8 * (i & 1)];
+          *reinterpret_cast<f32x4*>(dst) = f32x4{st.o[nt][0][i], st.o[nt][1][i], st.o[nt][2][i], st.o[nt][3][i]};
+          *reinterpret_cast<f32x4*>(dst + 4) = f32x4{st.o[nt][4][i], st.o[nt][5][i], st.o[nt][6][i], st.o[nt][7][i]};
+        }
+      __syncthreads();
+      if (half == 0) {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] += wt * sm.u.merge.o[w][r][d0 + e];
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm.r.stat.m[w][r]);
+        const float Mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          wt[w] = exp2f(sm.r.stat.m[w][r] - Mu);
+          Ls += wt[w] * sm.r.stat.l[w][r];
+          if constexpr (LSE) Lx += wt[w] * sm.r.stat.lx[w][r];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[half][e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int e = 0; e < kPer; e += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.u.o[w][r][local + e]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[half][e + k] += wt[w] * x[k];
+        }
     }
 
     const int row = rb * kRows + r;
     const bool row_valid = row < p.R;
     const int jrow = row_valid ? row / p.G : 0;
+    if (sm.nan_from[local >> 4] <= (gather ? 0x7FFFFFFE : L - p.nq + jrow)) {      // both halves lie in block local / 16
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[0][e] = acc[1][e] = __uint_as_float(0x7FC00000u);
+    }
     const int64_t orow = ((int64_t)s * p.nq + jrow) * p.Hq + g * p.G + (row_valid ? row - jrow * p.G : 0);
-    auto write_final = [&](float Mf, float Lf, float Lxf, const float (&a)[kPer]) {
+    auto write_final = [&](float Mf, float Lf, float Lxf, const float (&a)[2][kPer]) {
       if (!row_valid) return;
       const float inv = Lf == 0.f ? 0.f : 1.f / Lf;        // no visible key: 0
-      uint32_t w[kPer / 2];
 #pragma unroll
-      for (int e = 0; e < kPer; e += 2) w[e / 2] = pack_bf16x2(a[e] * inv, a[e + 1] * inv);
-      uint16_t* dst = p.out + orow * kD + d0;
+      for (int half = 0; half < 2; ++half) {
+        uint16_t* dst = p.out + orow * kD + d_at(half);
+        uint32_t w[kPer / 2];
 #pragma unroll
-      for (int e = 0; e < kPer / 8; ++e)
-        *reinterpret_cast<u32x4*>(dst + 8 * e) = u32x4{w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]};
-      if (p.lse && d0 == 0) p.lse[orow] = Lxf == 0.f ? -INFINITY : (Mf + __log2f(Lxf)) * kLn2;
+        for (int e = 0; e < kPer; e += 2) w[e / 2] = pack_bf16x2(a[half][e] * inv, a[half][e + 1] * inv);
+        if constexpr (kPer == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{w[0], w[1], w[2], w[3]};
+        else *reinterpret_cast<uint64_t*>(dst) = (uint64_t)w[0] | ((uint64_t)w[1] << 32);
+      }
+      if (LSE && local == 0) p.lse[orow] = Lxf == 0.f ? -INFINITY : (Mf + __log2f(Lxf)) * kLn2;
     };
 
     // ---- pieces of the unit: shares w0 .. w1
@@ -575,51 +664,59 @@ __global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
       const __amdgpu_buffer_rsrc_t rec = make_rsrc(p.part, p.part_bytes);
       // a share leaves at most two records: of a unit that began before it, and of one that goes on after it
       auto at = [&](int w) { return (uint32_t)(2 * (w * p.n_rb + rb) + (w == w0 ? 1 : 0)) * (uint32_t)(kRec * 4); };
-      auto store = [&](int w, float Mr, float Lr, float Lxr, const float (&a)[kPer]) {
+      constexpr int kWords = kPer / 2;                     // 16-byte words of a thread's outputs
+      auto store = [&](int w, float Mr, float Lr, float Lxr, const float (&a)[2][kPer]) {
         if (!row_valid) return;
-        if (d0 == 0) store16_coherent(rec, at(w) + 16 * r, f32x4{Mr, Lr, Lxr, 0.f});
+        if (local == 0) store16_coherent(rec, at(w) + 16 * r, f32x4{Mr, Lr, Lxr, 0.f});
 #pragma unroll
-        for (int c = 0; c < kPer / 4; ++c)
-          store16_coherent(rec, at(w) + 16 * kRows + 16 * (c * kThreads + tid),
-                           f32x4{a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]});
+        for (int c = 0; c < kWords; ++c) {
+          const float* x = &a[c / (kWords / 2)][4 * (c % (kWords / 2))];
+          store16_coherent(rec, at(w) + 16 * kRows + 16 * (c * kThreads + tid_m), f32x4{x[0], x[1], x[2], x[3]});
+        }
       };
-      float Mg, Lg, Lxg, ag[kPer];
+      float Mg, Lg, Lxg, ag[2][kPer];
       // records of shares first, first + step, ..., in that order, a batch of loads at a time
       auto merge = [&](int first, int count, int step) {
         Mg = -INFINITY;
         Lg = Lxg = 0.f;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) ag[e] = 0.f;
+        for (int e = 0; e < kPer; ++e) ag[0][e] = ag[1][e] = 0.f;
         if (!row_valid) return;
-        for (int k0 = 0; k0 < count; k0 += kGroup) {
-          f32x4 sv[kGroup], ov[kGroup][kPer / 4];
+        constexpr int kBatch = 4;                          // all loads of a batch are issued before any is used
+        for (int k0 = 0; k0 < count; k0 += kBatch) {
+          f32x4 sv[kBatch], ov[kBatch][kWords];
 #pragma unroll
-          for (int u = 0; u < kGroup; ++u) {
-            const bool ok = k0 + u < count;
-            const uint32_t a = at(first + (k0 + u) * step);
-            sv[u] = ok ? load16_coherent(rec, a + 16 * r) : f32x4{-INFINITY, 0.f, 0.f, 0.f};
+          for (int u = 0; u < kBatch; ++u) {
+            // past the last record: an address past the buffer, which reads as zeros
+            const uint32_t a = k0 + u < count ? at(first + (k0 + u) * step) : p.part_bytes;
+            sv[u] = load16_coherent(rec, a + 16 * r);
 #pragma unroll
-            for (int c = 0; c < kPer / 4; ++c)
-              ov[u][c] = ok ? load16_coherent(rec, a + 16 * kRows + 16 * (c * kThreads + tid)) : zero4();
+            for (int c = 0; c < kWords; ++c) ov[u][c] = load16_coherent(rec, a + 16 * kRows + 16 * (c * kThreads + tid_m));
           }
           float mb = Mg;
 #pragma unroll
-          for (int u = 0; u < kGroup; ++u) mb = fmaxf(mb, sv[u][0]);
+          for (int u = 0; u < kBatch; ++u) {
+            sv[u][0] = k0 + u < count ? sv[u][0] : -INFINITY;
+            mb = fmaxf(mb, sv[u][0]);
+          }
           const float mbu = mb == -INFINITY ? 0.f : mb;
           const float sc = exp2f(Mg - mbu);
           Lg *= sc;
           Lxg *= sc;
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) ag[e] *= sc;
+          for (int e = 0; e < kPer; ++e) {
+            ag[0][e] *= sc;
+            ag[1][e] *= sc;
+          }
 #pragma unroll
-          for (int u = 0; u < kGroup; ++u) {
-            const float wt = exp2f(sv[u][0] - mbu);
-            Lg += wt * sv[u][1];
-            Lxg += wt * sv[u][2];
+          for (int u = 0; u < kBatch; ++u) {
+            const float w = exp2f(sv[u][0] - mbu);
+            Lg += w * sv[u][1];
+            Lxg += w * sv[u][2];
 #pragma unroll
-            for (int c = 0; c < kPer / 4; ++c)
+            for (int c = 0; c < kWords; ++c)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) ag[4 * c + i] += wt * ov[u][c][i];
+              for (int k = 0; k < 4; ++k) ag[c / (kWords / 2)][4 * (c % (kWords / 2)) + k] += w * ov[u][c][k];
           }
           Mg = mb;
         }
@@ -668,20 +765,27 @@ __global__ __launch_bounds__(kThreads, 2) void qattn_kernel(QAttnParams p) {
     if (++g == p.Hkv) {
       g = 0;
       ++s;
-      n = unit_keys(p, s, L);
+      n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
+      L = __builtin_amdgcn_readfirstlane(L);
       T = unit_tiles(n);
     }
     __syncthreads();   // the merge buffer is read: the ring may be filled again
   }
 }
 
-template <int BITS, int NT>
+template <int BITS, int NT, bool LSE>
 hipError_t launch_rows(const QAttnParams& p, const QAttnPlan& pl, hipStream_t stream) {
   const dim3 grid((unsigned)pl.nblk), block(kThreads);
-  if (pl.rows == kQContiguous) hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQContiguous>), grid, block, 0, stream, p);
-  else if (pl.rows == kQPages) hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQPages>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQTable>), grid, block, 0, stream, p);
+  if (pl.rows == kQContiguous) hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQContiguous, LSE>), grid, block, 0, stream, p);
+  else if (pl.rows == kQPages) hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQPages, LSE>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQTable, LSE>), grid, block, 0, stream, p);
   return hipGetLastError();
+}
+
+template <int BITS>
+hipError_t launch_bits(const QAttnParams& p, const QAttnPlan& pl, hipStream_t stream) {
+  if (pl.nt == 1) return p.lse ? launch_rows<BITS, 1, true>(p, pl, stream) : launch_rows<BITS, 1, false>(p, pl, stream);
+  return p.lse ? launch_rows<BITS, 2, true>(p, pl, stream) : launch_rows<BITS, 2, false>(p, pl, stream);
 }
 
 }  // namespace
@@ -692,8 +796,7 @@ QAttnPlan plan_qattn(int S, int Hkv, int Hq, int nq, int64_t entries, bool gathe
   pl.R = (int)(R < (1 << 30) ? R : (1 << 30));
   pl.nt = R <= 16 ? 1 : 2;
   pl.n_rb = (pl.R + 16 * pl.nt - 1) / (16 * pl.nt);
-  // the kernel's page division is exact for 16-row sub-tiles numbered below 2^22
-  pl.rows = gather ? kQTable : !paged ? kQContiguous : page_size % 16 == 0 && entries <= (1 << 26) - 64 ? kQPages : kQTable;
+  pl.rows = gather ? kQTable : !paged ? kQContiguous : page_size % 16 == 0 ? kQPages : kQTable;
   pl.min_share = 8;
   const int64_t tiles = (int64_t)S * Hkv * (entries > 0 ? (entries + kTile - 1) / kTile : 1);
   int64_t nW = (tiles + pl.min_share - 1) / pl.min_share;
@@ -709,8 +812,7 @@ QAttnPlan plan_qattn(int S, int Hkv, int Hq, int nq, int64_t entries, bool gathe
 }
 
 hipError_t launch_qattn(const QAttnParams& p, const QAttnPlan& pl, int bits, hipStream_t stream) {
-  if (bits == 4) return pl.nt == 1 ? launch_rows<4, 1>(p, pl, stream) : launch_rows<4, 2>(p, pl, stream);
-  return pl.nt == 1 ? launch_rows<8, 1>(p, pl, stream) : launch_rows<8, 2>(p, pl, stream);
+  return bits == 4 ? launch_bits<4>(p, pl, stream) : launch_bits<8>(p, pl, stream);
 }
 
 }  // namespace bd
