@@ -574,14 +574,43 @@ def bd_sample_budgets(u: torch.Tensor, budgets, weights) -> torch.Tensor:
 
 # --------------------------------------------------------------------- caches held in 8 or 4 bits
 
-class QuantKV(NamedTuple):
-    """A KV cache held in 8 or 4 bits: uint8 codes [S, Hkv, L, 128 or 64] (contiguous) or
-    [num_pages, Hkv, page_size, 128 or 64] (paged) and uint8 scales of the same rows, [.., .., .., 4].  K and V
-    share strides, and the scales' strides are the codes' in rows (bd_qkv_desc describes the format)."""
+class _QuantTensors(NamedTuple):
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor
     v_scale: torch.Tensor
+
+
+class QuantKV(_QuantTensors):
+    """A KV cache held in 8 or 4 bits: uint8 codes [S, Hkv, L, 128 or 64] (contiguous) or
+    [num_pages, Hkv, page_size, 128 or 64] (paged) and uint8 scales of the same rows, [.., .., .., 4].  K and V
+    share strides, and the scales' strides are the codes' in rows (bd_qkv_desc describes the format).
+
+    A handle to keep: shapes and strides are looked at once, at its first use, so the tensors' geometry must not be
+    changed in place afterwards (their contents are what the operations read and write)."""
+
+    def geometry(self):
+        """(bits, dim 0, Hkv, rows, strides of the three in rows, device index), checked."""
+        k, v, ks, vs = self
+        sh, st = k.shape, k.stride()
+        if not (k.dtype == _U8 and len(sh) == 4 and (sh[3] == 128 or sh[3] == 64) and st[3] == 1):
+            raise BdError(BD_ERR_INVALID_ARG, "k must be uint8 codes [*, Hkv, *, 128 or 64] with a contiguous last dimension")
+        if not (v.dtype == _U8 and v.shape == sh and v.stride() == st):
+            raise BdError(BD_ERR_INVALID_ARG, "v must match k in shape and strides")
+        w, (n0, hkv, n2, _), sst = sh[3], sh, ks.stride()
+        if not (ks.dtype == _U8 and vs.dtype == _U8 and ks.shape == (n0, hkv, n2, 4) and vs.shape == ks.shape
+                and sst[3] == 1 and vs.stride() == sst):
+            raise BdError(BD_ERR_INVALID_ARG, "k_scale and v_scale must be uint8 [*, Hkv, *, 4] with equal strides")
+        for i in (0, 1, 2):      # a dimension of one has no stride to speak of
+            if sh[i] > 1 and not (st[i] % w == 0 and sst[i] == 4 * (st[i] // w)):
+                raise BdError(BD_ERR_INVALID_ARG, "code and scale strides must be the same whole numbers of rows")
+        dev = k.get_device()
+        if v.get_device() != dev or ks.get_device() != dev or vs.get_device() != dev:
+            raise BdError(BD_ERR_INVALID_ARG, "a cache's tensors must be on one device")
+        self._geometry = (w // 16, n0, hkv, n2, st[0] // w, st[1] // w, st[2] // w, dev)
+        return self._geometry
+
+    _geometry = None
 
 
 def quant_kv_empty(n: int, num_kv_heads: int, rows: int, bits: int, device="cuda") -> QuantKV:
@@ -592,45 +621,32 @@ def quant_kv_empty(n: int, num_kv_heads: int, rows: int, bits: int, device="cuda
 
 
 _U8 = torch.uint8
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
 
 
 def _qkv(cache, seq_lens, page_table=None, max_seq_len=None):
-    """The bytes of a QkvDesc for these tensors (checked), and its (num_seqs, num_kv_heads, max_seq_len)."""
-    k, v, ks, vs = cache
-    sh, st = k.shape, k.stride()
-    if not (k.dtype == _U8 and len(sh) == 4 and (sh[3] == 128 or sh[3] == 64) and st[3] == 1):
-        raise BdError(BD_ERR_INVALID_ARG, "k must be uint8 codes [*, Hkv, *, 128 or 64] with a contiguous last dimension")
-    if not (v.dtype == _U8 and v.shape == sh and v.stride() == st):
-        raise BdError(BD_ERR_INVALID_ARG, "v must match k in shape and strides")
-    w, (n0, hkv, n2, _) = sh[3], sh
-    if not (ks.dtype == _U8 and vs.dtype == _U8 and ks.shape == (n0, hkv, n2, 4) and vs.shape == ks.shape
-            and ks.stride(3) == 1 and vs.stride() == ks.stride()):
-        raise BdError(BD_ERR_INVALID_ARG, "k_scale and v_scale must be uint8 [*, Hkv, *, 4] with equal strides")
-    rows = (st[0] // w, st[1] // w, st[2] // w)
-    sst = ks.stride()
-    for i in (0, 1, 2):          # a dimension of one has no stride to speak of
-        if sh[i] > 1 and not (st[i] % w == 0 and sst[i] == 4 * rows[i]):
-            raise BdError(BD_ERR_INVALID_ARG, "code and scale strides must be the same whole numbers of rows")
+    """The bytes of a QkvDesc for these tensors (checked), and its (num_seqs, num_kv_heads, max_seq_len, device)."""
+    bits, n0, hkv, n2, s0, s1, s2, dev = cache._geometry or cache.geometry()
     ls = seq_lens.shape
     if not (seq_lens.dtype == _I32T and len(ls) == 1 and seq_lens.is_contiguous()):
         raise BdError(BD_ERR_INVALID_ARG, "seq_lens must be contiguous int32 [S]")
     S = ls[0]
-    if page_table is None:
-        if n0 != S:
-            raise BdError(BD_ERR_INVALID_ARG, "contiguous k must be [S, Hkv, L, 128 or 64]")
-        L = n2 if max_seq_len is None else int(max_seq_len)
-        if L > n2:
-            raise BdError(BD_ERR_INVALID_ARG, "max_seq_len exceeds the cache's rows")
-        geom = (0, 0, 0, seq_lens.data_ptr(), 0, rows[0], rows[1], rows[2], 0)
-    else:
+    try:
+        if page_table is None:
+            if n0 != S:
+                raise BdError(BD_ERR_INVALID_ARG, "contiguous k must be [S, Hkv, L, 128 or 64]")
+            L = n2 if max_seq_len is None else int(max_seq_len)
+            if L > n2:
+                raise BdError(BD_ERR_INVALID_ARG, "max_seq_len exceeds the cache's rows")
+            return _QKV_BYTES.pack(cache[0].data_ptr(), cache[1].data_ptr(), cache[2].data_ptr(), cache[3].data_ptr(), bits, S,
+                                   hkv, HEAD_DIM, L, 0, 0, 0, seq_lens.data_ptr(), 0, s0, s1, s2, 0), S, hkv, L, dev
         ps = page_table.shape
         if not (page_table.dtype == _I32T and len(ps) == 2 and ps[0] == S and page_table.is_contiguous()):
             raise BdError(BD_ERR_INVALID_ARG, "page_table must be contiguous int32 [S, max_pages]")
         L = ps[1] * n2 if max_seq_len is None else int(max_seq_len)
-        geom = (n2, ps[1], n0, seq_lens.data_ptr(), page_table.data_ptr(), 0, rows[1], rows[2], rows[0])
-    try:
-        return _QKV_BYTES.pack(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), w // 16, S, hkv, HEAD_DIM, L,
-                               *geom), S, hkv, L
+        return _QKV_BYTES.pack(cache[0].data_ptr(), cache[1].data_ptr(), cache[2].data_ptr(), cache[3].data_ptr(), bits, S,
+                               hkv, HEAD_DIM, L, n2, ps[1], n0, seq_lens.data_ptr(), page_table.data_ptr(), 0, s1, s2,
+                               s0), S, hkv, L, dev
     except struct.error:
         raise BdError(BD_ERR_UNSUPPORTED, "a size of the cache is beyond 32 bits") from None
 
@@ -641,9 +657,11 @@ def qkv_desc(cache: QuantKV, seq_lens: torch.Tensor, page_table: Optional[torch.
     return QkvDesc.from_buffer_copy(_qkv(cache, seq_lens, page_table, max_seq_len)[0])
 
 
-def _here(*tensors) -> None:
-    """Every tensor (None aside) lies on the current GPU, whose stream the call is issued on."""
-    dev = _get_device() if _get_device is not None and torch.cuda.is_initialized() else 0
+def _here(dev: int, *tensors) -> None:
+    """The cache's device `dev` is the current GPU, whose stream the call is issued on, and every tensor is on it."""
+    now = _get_device() if _get_device is not None and torch.cuda.is_initialized() else 0
+    if dev != now:
+        raise BdError(BD_ERR_INVALID_ARG, f"the cache must be on the current GPU ({now}), not on device {dev}")
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise BdError(BD_ERR_INVALID_ARG, f"tensors must be on the current GPU ({dev}), not on {t.device}")
@@ -652,7 +670,7 @@ def _here(*tensors) -> None:
 def _ws_q(op: str, nbytes: int, like: torch.Tensor, stream: int, workspace: Optional[Workspace]):
     """As _ws, but a graph under capture gets scratch of its own (cleared by the graph itself) unless the caller
     gives a workspace: two graphs that shared a default one could be replayed side by side."""
-    if workspace is None and torch.cuda.is_current_stream_capturing():
+    if workspace is None and _capturing():
         workspace = Workspace()
     return _ws(op, nbytes, like, stream, workspace)
 
@@ -664,21 +682,22 @@ def bd_cache_append_q(cache: QuantKV, seq_lens: torch.Tensor, k_new: torch.Tenso
     """Append rows in place, quantised as they are written: k_new, v_new bf16 [S, n, Hkv, 128] go to positions
     seq_lens[s] .. (the first counts[s] of them with counts int32 [S]); seq_lens (and, with the sparse list
     idx [S, Hkv, ld] / nsel [S], the list) advance in place."""
-    kv, S, hkv, _ = _qkv(cache, seq_lens, page_table, max_seq_len)
+    kv, S, hkv, _, dev = _qkv(cache, seq_lens, page_table, max_seq_len)
     ns = k_new.shape
-    _require(k_new.dtype == _BF16 and len(ns) == 4 and k_new.is_contiguous() and v_new.shape == ns and v_new.is_contiguous()
-             and v_new.dtype == _BF16 and ns[0] == S and ns[2] == hkv and ns[3] == HEAD_DIM,
-             "k_new and v_new must be contiguous bf16 [S,n,Hkv,128]")
-    _require(counts is None or (counts.dtype == _I32T and counts.shape == (S,) and counts.is_contiguous()), "counts must be int32 [S]")
+    if not (k_new.dtype == _BF16 and len(ns) == 4 and k_new.is_contiguous() and v_new.shape == ns and v_new.is_contiguous()
+            and v_new.dtype == _BF16 and ns[0] == S and ns[2] == hkv and ns[3] == HEAD_DIM):
+        raise BdError(BD_ERR_INVALID_ARG, "k_new and v_new must be contiguous bf16 [S,n,Hkv,128]")
+    if counts is not None:
+        _require(counts.dtype == _I32T and counts.shape == (S,) and counts.is_contiguous(), "counts must be int32 [S]")
     _require((idx is None) == (nsel is None), "idx and nsel go together")
     ld = 0
     if idx is not None:
         ld = idx.shape[-1]
         _require(idx.dtype == _I32T and idx.shape == (S, hkv, ld) and idx.is_contiguous(), "idx must be contiguous int32 [S,Hkv,ld]")
         _require(nsel.dtype == _I32T and nsel.shape == (S,) and nsel.is_contiguous(), "nsel must be int32 [S]")
-    _here(*cache, seq_lens, k_new, v_new, counts, idx, nsel, page_table)
-    _check(_packed_lib().bd_cache_append_q(kv, k_new.data_ptr(), v_new.data_ptr(), ns[1], _ptr(counts), _ptr(idx), ld,
-                                           _ptr(nsel), _stream()))
+    _here(dev, seq_lens, k_new, v_new, counts, idx, nsel, page_table)
+    _check((_packed or _packed_lib()).bd_cache_append_q(kv, k_new.data_ptr(), v_new.data_ptr(), ns[1], _ptr(counts),
+                                                        _ptr(idx), ld, _ptr(nsel), _stream()))
 
 
 def bd_cache_read_q(cache: QuantKV, seq_lens: torch.Tensor, n: int, *, first: Optional[torch.Tensor] = None,
@@ -687,9 +706,10 @@ def bd_cache_read_q(cache: QuantKV, seq_lens: torch.Tensor, n: int, *, first: Op
     """Rows first[s] .. first[s]+n-1 (first None: 0) of every (sequence, KV head) as bf16 (k, v) [S, Hkv, n, 128]; rows
     that the cache does not hold are zero.  with_v=False: (k, None), as the selections need.  outputs: optional
     preallocated (k, v), of equal strides with a contiguous last dimension (a part of a larger bf16 cache, say)."""
-    kv, S, hkv, _ = _qkv(cache, seq_lens, page_table, max_seq_len)
+    kv, S, hkv, _, dev = _qkv(cache, seq_lens, page_table, max_seq_len)
     _require(n >= 0, "n must not be negative")
-    _require(first is None or (first.dtype == _I32T and first.shape == (S,) and first.is_contiguous()), "first must be int32 [S]")
+    if first is not None:
+        _require(first.dtype == _I32T and first.shape == (S,) and first.is_contiguous(), "first must be int32 [S]")
     shape = (S, hkv, n, HEAD_DIM)
     ko, vo = (tuple(outputs) + (None, None))[:2] if outputs is not None else (None, None)
     if ko is None:
@@ -697,12 +717,14 @@ def bd_cache_read_q(cache: QuantKV, seq_lens: torch.Tensor, n: int, *, first: Op
     if not with_v:
         vo = None
     elif vo is None:
-        vo = torch.empty_strided(shape, ko.stride(), dtype=_BF16, device=ko.device)
+        vo = torch.empty_like(ko) if outputs is None else torch.empty_strided(shape, ko.stride(), dtype=_BF16, device=ko.device)
     st = ko.stride()
-    _require(ko.dtype == _BF16 and ko.shape == shape and st[3] == 1, "k output must be bf16 [S,Hkv,n,128]")
-    _require(vo is None or (vo.dtype == _BF16 and vo.shape == shape and vo.stride() == st), "v output must match k's")
-    _here(*cache, seq_lens, first, ko, vo, page_table)
-    _check(_packed_lib().bd_cache_read_q(kv, _ptr(first), n, ko.data_ptr(), _ptr(vo), st[0], st[1], st[2], _stream()))
+    if outputs is not None:
+        _require(ko.dtype == _BF16 and ko.shape == shape and st[3] == 1, "k output must be bf16 [S,Hkv,n,128]")
+        _require(vo is None or (vo.dtype == _BF16 and vo.shape == shape and vo.stride() == st), "v output must match k's")
+    _here(dev, seq_lens, first, ko, vo, page_table)
+    _check((_packed or _packed_lib()).bd_cache_read_q(kv, _ptr(first), n, ko.data_ptr(), _ptr(vo), st[0], st[1], st[2],
+                                                      _stream()))
     return ko, vo
 
 
@@ -713,7 +735,7 @@ def bd_sparse_decode_attn_q(cache: QuantKV, q: torch.Tensor, idx: torch.Tensor, 
                             workspace: Optional[Workspace] = None):
     """Drafter decode attention over selected entries of a quantised cache.  q: bf16 [S, Hq, 128]; idx int32
     [S, Hkv, ld].  out / lse: optional preallocated outputs."""
-    kv, S, hkv, _ = _qkv(cache, seq_lens, page_table, max_seq_len)
+    kv, S, hkv, _, dev = _qkv(cache, seq_lens, page_table, max_seq_len)
     qs, xs = q.shape, idx.shape
     if not (q.dtype == _BF16 and len(qs) == 3 and q.is_contiguous() and qs[0] == S and qs[2] == HEAD_DIM):
         raise BdError(BD_ERR_INVALID_ARG, "q must be contiguous bf16 [S,Hq,128]")
@@ -722,13 +744,13 @@ def bd_sparse_decode_attn_q(cache: QuantKV, q: torch.Tensor, idx: torch.Tensor, 
     if not (nsel.dtype == _I32T and nsel.shape == (S,) and nsel.is_contiguous()):
         raise BdError(BD_ERR_INVALID_ARG, "nsel must be int32 [S]")
     Hq, ld = qs[1], xs[2]
-    out = _out_like(out, q, "out")
+    out = torch.empty_like(q) if out is None else _out(out, qs, _BF16, q, "out")
     lse = _out(lse, (S, Hq), _F32T, q, "lse") if return_lse else None
-    _here(*cache, q, idx, nsel, seq_lens, page_table, out, lse)
+    _here(dev, q, idx, nsel, seq_lens, page_table, out, lse)
     stream = _stream()
     wp, wb = _ws_q("decode_q", _ws_bytes("bd_sparse_decode_attn_q_workspace_bytes", S, hkv, Hq, ld), q, stream, workspace)
-    _check(_packed_lib().bd_sparse_decode_attn_q(kv, q.data_ptr(), Hq, idx.data_ptr(), ld, nsel.data_ptr(), _scale(scale),
-                                                 out.data_ptr(), _ptr(lse), wp, wb, stream))
+    _check((_packed or _packed_lib()).bd_sparse_decode_attn_q(kv, q.data_ptr(), Hq, idx.data_ptr(), ld, nsel.data_ptr(),
+                                                              _scale(scale), out.data_ptr(), _ptr(lse), wp, wb, stream))
     return (out, lse) if return_lse else out
 
 
@@ -738,16 +760,16 @@ def bd_verify_attn_q(cache: QuantKV, q: torch.Tensor, seq_lens: torch.Tensor, *,
                      lse: Optional[torch.Tensor] = None, workspace: Optional[Workspace] = None):
     """Verifier attention at the gamma+1 draft positions over a quantised cache.  q: bf16 [S, gamma+1, Hq, 128]
     (gamma = 0: a single-token decode over the whole cache).  out / lse: optional preallocated outputs."""
-    kv, S, hkv, L = _qkv(cache, seq_lens, page_table, max_seq_len)
+    kv, S, hkv, L, dev = _qkv(cache, seq_lens, page_table, max_seq_len)
     qs = q.shape
     if not (q.dtype == _BF16 and len(qs) == 4 and q.is_contiguous() and qs[0] == S and qs[3] == HEAD_DIM):
         raise BdError(BD_ERR_INVALID_ARG, "q must be contiguous bf16 [S,gamma+1,Hq,128]")
     _, R, Hq, _ = qs
-    out = _out_like(out, q, "out")
+    out = torch.empty_like(q) if out is None else _out(out, qs, _BF16, q, "out")
     lse = _out(lse, (S, R, Hq), _F32T, q, "lse") if return_lse else None
-    _here(*cache, q, seq_lens, page_table, out, lse)
+    _here(dev, q, seq_lens, page_table, out, lse)
     stream = _stream()
     wp, wb = _ws_q("verify_q", _ws_bytes("bd_verify_attn_q_workspace_bytes", S, hkv, Hq, R - 1, L), q, stream, workspace)
-    _check(_packed_lib().bd_verify_attn_q(kv, q.data_ptr(), Hq, R - 1, _scale(scale), out.data_ptr(), _ptr(lse), wp, wb,
-                                          stream))
+    _check((_packed or _packed_lib()).bd_verify_attn_q(kv, q.data_ptr(), Hq, R - 1, _scale(scale), out.data_ptr(),
+                                                       _ptr(lse), wp, wb, stream))
     return (out, lse) if return_lse else out

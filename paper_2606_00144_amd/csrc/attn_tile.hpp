@@ -45,6 +45,25 @@ __device__ inline void dma16_hidden(const uint16_t* base, uint32_t voff, uint32_
       : "s"(lds), "v"(voff), "s"(base)
       : "memory", "m0");
 }
+// Both with the non-temporal policy.
+__device__ inline void dma16_nt_hidden(const uint16_t* g, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n"
+      "s_nop 0\n"
+      "global_load_lds_dwordx4 %1, off nt"
+      :
+      : "s"(lds), "v"(g)
+      : "memory", "m0");
+}
+__device__ inline void dma16_nt_hidden(const uint16_t* base, uint32_t voff, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n"
+      "s_nop 0\n"
+      "global_load_lds_dwordx4 %1, %2 nt"
+      :
+      : "s"(lds), "v"(voff), "s"(base)
+      : "memory", "m0");
+}
 // One 4-byte load a lane: lane l's bytes land at the LDS address + 4*l.
 __device__ inline void dma4_hidden(const void* g, uint32_t lds) {
   asm volatile(

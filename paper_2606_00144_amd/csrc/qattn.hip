@@ -69,7 +69,7 @@ constexpr int kMaxBlocks = 512;                // workgroups of a launch
 template <int BITS, int NT, int ROWS>
 struct Config {
   static constexpr int kPerCu = BITS == 8 || NT == 2 ? 2 : 3;
-  static constexpr int kTab = ROWS == kQContiguous ? 4 : ROWS == kQPages ? (BITS == 4 && NT == 1 ? 384 : 448) : BITS == 8 ? 1024 : 2048;
+  static constexpr int kTab = ROWS == kQContiguous ? 4 : ROWS == kQPages ? 448 : BITS == 8 || NT == 2 ? 1024 : 2048;
 };
 
 template <int BITS, int NT, int ROWS>
@@ -77,7 +77,7 @@ struct Smem {
   alignas(16) uint32_t tab[Config<BITS, NT, ROWS>::kTab];
   union {
     alignas(64) uint8_t ring[kWaves][kRing][Tile<BITS>::kBytes];
-    float o[kWaves][16 * NT][kD / 2 + 4];      // half of the head dimension: the waves' states, when they merge
+    float o[kWaves][16 * NT][kD + 4];          // the waves' states, when they merge
   } u;
   union {
     alignas(64) uint8_t q[16 * NT][kD * 2];    // query rows, chunk c (16 bytes) of row r at position c ^ k_swizzle(r % 16)
@@ -503,8 +503,8 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
                   ko = (uint32_t)kr * tok_bytes + 16u * (uint32_t)TL::k_chunk(lane_i, e);
                   vo = (uint32_t)vr * tok_bytes + 16u * (uint32_t)TL::v_chunk(lane_i);
                 }
-                dma16_hidden(reinterpret_cast<const uint16_t*>(kb), ko, to);
-                dma16_hidden(reinterpret_cast<const uint16_t*>(vb), vo, to + TL::kV);
+                dma16_nt_hidden(reinterpret_cast<const uint16_t*>(kb), ko, to);
+                dma16_nt_hidden(reinterpret_cast<const uint16_t*>(vb), vo, to + TL::kV);
               }
             }
             const int lane_s = here(lane);                 // three instructions a tile rather than three registers
@@ -528,6 +528,10 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       }
+      // The second workgroup of a CU runs its first half at a raised priority: issue prefers the older waves, which
+      // would be done early and leave the younger ones alone, one a SIMD (16K x 8 in 4 bits 41.0 -> 39.0 us, 8 bits
+      // 54.7 -> 53.0; raised throughout 40.0 and 53.7).
+      if (blockIdx.x >= kCus) __builtin_amdgcn_s_setprio(1);
       int i = 0, slot = 0;
       // tile i of this wave: its codes to registers, its slot filled again, the products
       auto step = [&](auto dirty_tag) {
@@ -535,6 +539,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
         const int c = c0 + wave + i * kWaves;
         if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TL::kLoads) : "memory");   // the next tile is on its way
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (2 * i == mine || 2 * i == mine - 1) __builtin_amdgcn_s_setprio(0);
         const bool more = i + kRing < mine;
         const Where next = where(more ? c + kRing * kWaves : c);
         TileRegs<BITS> tile;
@@ -569,17 +574,15 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       const int clean = first_dirty > c0 + wave ? (first_dirty - c0 - wave + kWaves - 1) / kWaves : 0;
       while (i < mine && i < clean) step(BoolTag<false>{});
       while (i < mine) step(BoolTag<true>{});
+      __builtin_amdgcn_s_setprio(0);
       c0 = c1;
       if (ROWS != kQContiguous && c0 < tn) __syncthreads();   // the table is filled again
     }
 
-    // ---- the four waves' states, through LDS, half of the head dimension at a time.  Thread -> row r and kPer
-    // outputs of each half: those at local .. of the half, which lie at d_at(half) ..
-    constexpr int kPer = kRows * kD / 2 / kThreads;        // 4 or 8
+    // ---- the four waves' states, through LDS.  Thread -> row r and the kPer outputs from d0 on
+    constexpr int kPer = kRows * kD / kThreads;            // 8 or 16
     const int tid_m = here(tid), lgm = (tid_m >> 4) & 3, lrm = tid_m & 15;
-    const int r = tid_m / (kD / 2 / kPer), local = (tid_m % (kD / 2 / kPer)) * kPer;
-    auto d_at = [&](int half) { return 32 * (local >> 4) + 16 * half + (local & 15); };
-    float M = -INFINITY, Ls = 0.f, Lx = 0.f, acc[2][kPer];
+    const int r = tid_m / (kD / kPer), d0 = (tid_m % (kD / kPer)) * kPer;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the query rows of a piece without keys
     __syncthreads();
 #pragma unroll
@@ -596,64 +599,51 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
         sm.r.stat.l[wave][16 * nt + lrm] = l;
         sm.r.stat.lx[wave][16 * nt + lrm] = lx;
       }
-    }
-    float wt[kWaves];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      if (half == 1) __syncthreads();
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 2 * half; i < 2 * half + 2; ++i) {
-          float* dst = &sm.u.o[wave][16 * nt + lrm][16 * lgm + 8 * (i & 1)];
-          *reinterpret_cast<f32x4*>(dst) = f32x4{st.o[nt][0][i], st.o[nt][1][i], st.o[nt][2][i], st.o[nt][3][i]};
-          *reinterpret_cast<f32x4*>(dst + 4) = f32x4{st.o[nt][4][i], st.o[nt][5][i], st.o[nt][6][i], st.o[nt][7][i]};
-        }
-      __syncthreads();
-      if (half == 0) {
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm.r.stat.m[w][r]);
-        const float Mu = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          wt[w] = exp2f(sm.r.stat.m[w][r] - Mu);
-          Ls += wt[w] * sm.r.stat.l[w][r];
-          if constexpr (LSE) Lx += wt[w] * sm.r.stat.lx[w][r];
-        }
+      for (int i = 0; i < 4; ++i) {
+        float* dst = &sm.u.o[wave][16 * nt + lrm][32 * lgm + 8 * i];
+        *reinterpret_cast<f32x4*>(dst) = f32x4{st.o[nt][0][i], st.o[nt][1][i], st.o[nt][2][i], st.o[nt][3][i]};
+        *reinterpret_cast<f32x4*>(dst + 4) = f32x4{st.o[nt][4][i], st.o[nt][5][i], st.o[nt][6][i], st.o[nt][7][i]};
       }
+    }
+    __syncthreads();
+    float M = -INFINITY, Ls = 0.f, Lx = 0.f, acc[kPer];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[half][e] = 0.f;
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm.r.stat.m[w][r]);
+    const float Mu = M == -INFINITY ? 0.f : M;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w)
+    for (int e = 0; e < kPer; ++e) acc[e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < kPer; e += 4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.u.o[w][r][local + e]);
+    for (int w = 0; w < kWaves; ++w) {
+      const float wt = exp2f(sm.r.stat.m[w][r] - Mu);
+      Ls += wt * sm.r.stat.l[w][r];
+      if constexpr (LSE) Lx += wt * sm.r.stat.lx[w][r];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) acc[half][e + k] += wt[w] * x[k];
-        }
+      for (int e = 0; e < kPer; e += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.u.o[w][r][d0 + e]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[e + k] += wt * x[k];
+      }
     }
 
     const int row = rb * kRows + r;
     const bool row_valid = row < p.R;
     const int jrow = row_valid ? row / p.G : 0;
-    if (sm.nan_from[local >> 4] <= (gather ? 0x7FFFFFFE : L - p.nq + jrow)) {      // both halves lie in block local / 16
+    if (sm.nan_from[d0 >> 5] <= (gather ? 0x7FFFFFFE : L - p.nq + jrow)) {         // a thread's outputs lie in one block
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[0][e] = acc[1][e] = __uint_as_float(0x7FC00000u);
+      for (int e = 0; e < kPer; ++e) acc[e] = __uint_as_float(0x7FC00000u);
     }
     const int64_t orow = ((int64_t)s * p.nq + jrow) * p.Hq + g * p.G + (row_valid ? row - jrow * p.G : 0);
-    auto write_final = [&](float Mf, float Lf, float Lxf, const float (&a)[2][kPer]) {
+    auto write_final = [&](float Mf, float Lf, float Lxf, const float (&a)[kPer]) {
       if (!row_valid) return;
       const float inv = Lf == 0.f ? 0.f : 1.f / Lf;        // no visible key: 0
+      uint16_t* dst = p.out + orow * kD + d0;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint16_t* dst = p.out + orow * kD + d_at(half);
-        uint32_t w[kPer / 2];
-#pragma unroll
-        for (int e = 0; e < kPer; e += 2) w[e / 2] = pack_bf16x2(a[half][e] * inv, a[half][e + 1] * inv);
-        if constexpr (kPer == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{w[0], w[1], w[2], w[3]};
-        else *reinterpret_cast<uint64_t*>(dst) = (uint64_t)w[0] | ((uint64_t)w[1] << 32);
-      }
-      if (LSE && local == 0) p.lse[orow] = Lxf == 0.f ? -INFINITY : (Mf + __log2f(Lxf)) * kLn2;
+      for (int e = 0; e < kPer; e += 8)
+        *reinterpret_cast<u32x4*>(dst + e) =
+            u32x4{pack_bf16x2(a[e] * inv, a[e + 1] * inv), pack_bf16x2(a[e + 2] * inv, a[e + 3] * inv),
+                  pack_bf16x2(a[e + 4] * inv, a[e + 5] * inv), pack_bf16x2(a[e + 6] * inv, a[e + 7] * inv)};
+      if (LSE && d0 == 0) p.lse[orow] = Lxf == 0.f ? -INFINITY : (Mf + __log2f(Lxf)) * kLn2;
     };
 
     // ---- pieces of the unit: shares w0 .. w1
@@ -664,34 +654,32 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       const __amdgpu_buffer_rsrc_t rec = make_rsrc(p.part, p.part_bytes);
       // a share leaves at most two records: of a unit that began before it, and of one that goes on after it
       auto at = [&](int w) { return (uint32_t)(2 * (w * p.n_rb + rb) + (w == w0 ? 1 : 0)) * (uint32_t)(kRec * 4); };
-      constexpr int kWords = kPer / 2;                     // 16-byte words of a thread's outputs
-      auto store = [&](int w, float Mr, float Lr, float Lxr, const float (&a)[2][kPer]) {
+      auto store = [&](int w, float Mr, float Lr, float Lxr, const float (&a)[kPer]) {
         if (!row_valid) return;
-        if (local == 0) store16_coherent(rec, at(w) + 16 * r, f32x4{Mr, Lr, Lxr, 0.f});
+        if (d0 == 0) store16_coherent(rec, at(w) + 16 * r, f32x4{Mr, Lr, Lxr, 0.f});
 #pragma unroll
-        for (int c = 0; c < kWords; ++c) {
-          const float* x = &a[c / (kWords / 2)][4 * (c % (kWords / 2))];
-          store16_coherent(rec, at(w) + 16 * kRows + 16 * (c * kThreads + tid_m), f32x4{x[0], x[1], x[2], x[3]});
-        }
+        for (int c = 0; c < kPer / 4; ++c)
+          store16_coherent(rec, at(w) + 16 * kRows + 16 * (c * kThreads + tid_m),
+                           f32x4{a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]});
       };
-      float Mg, Lg, Lxg, ag[2][kPer];
+      float Mg, Lg, Lxg, ag[kPer];
       // records of shares first, first + step, ..., in that order, a batch of loads at a time
       auto merge = [&](int first, int count, int step) {
         Mg = -INFINITY;
         Lg = Lxg = 0.f;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) ag[0][e] = ag[1][e] = 0.f;
+        for (int e = 0; e < kPer; ++e) ag[e] = 0.f;
         if (!row_valid) return;
-        constexpr int kBatch = 4;                          // all loads of a batch are issued before any is used
+        constexpr int kBatch = NT == 1 ? 8 : 4;            // all loads of a batch are issued before any is used
         for (int k0 = 0; k0 < count; k0 += kBatch) {
-          f32x4 sv[kBatch], ov[kBatch][kWords];
+          f32x4 sv[kBatch], ov[kBatch][kPer / 4];
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) {
             // past the last record: an address past the buffer, which reads as zeros
             const uint32_t a = k0 + u < count ? at(first + (k0 + u) * step) : p.part_bytes;
             sv[u] = load16_coherent(rec, a + 16 * r);
 #pragma unroll
-            for (int c = 0; c < kWords; ++c) ov[u][c] = load16_coherent(rec, a + 16 * kRows + 16 * (c * kThreads + tid_m));
+            for (int c = 0; c < kPer / 4; ++c) ov[u][c] = load16_coherent(rec, a + 16 * kRows + 16 * (c * kThreads + tid_m));
           }
           float mb = Mg;
 #pragma unroll
@@ -704,19 +692,16 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
           Lg *= sc;
           Lxg *= sc;
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) {
-            ag[0][e] *= sc;
-            ag[1][e] *= sc;
-          }
+          for (int e = 0; e < kPer; ++e) ag[e] *= sc;
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) {
             const float w = exp2f(sv[u][0] - mbu);
             Lg += w * sv[u][1];
             Lxg += w * sv[u][2];
 #pragma unroll
-            for (int c = 0; c < kWords; ++c)
+            for (int c = 0; c < kPer / 4; ++c)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) ag[c / (kWords / 2)][4 * (c % (kWords / 2)) + k] += w * ov[u][c][k];
+              for (int k = 0; k < 4; ++k) ag[4 * c + k] += w * ov[u][c][k];
           }
           Mg = mb;
         }

@@ -22,6 +22,10 @@ constexpr int kGroupRows = 64;                 // rows of one head that a workgr
 
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
+// The new rows are read once, the rows read back go to a buffer larger than the caches: non-temporal.
+__device__ inline u32x4 load16_nt(const uint16_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+__device__ inline void store16_nt(uint16_t* p, const u32x4& v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p)); }
+
 template <int CTRL>
 __device__ inline uint32_t max_dpp(uint32_t x) {
   const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
@@ -70,15 +74,23 @@ __device__ inline int quantise8(const u32x4& w, uint32_t (&c)[2]) {
   return byte;
 }
 
-// This lane's part (elements 8*j .. 8*j+7) of row `row` from 16 bytes of bf16 at src.
+// The scale bytes of a row's four quads in one word, in every lane of the 16.
+template <int CTRL>
+__device__ inline uint32_t or_dpp(uint32_t x) { return x | (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
+__device__ inline uint32_t row_scales(int byte, int j) {
+  const uint32_t x = (uint32_t)byte << (8 * (j >> 2));
+  return or_dpp<0x128>(or_dpp<0x124>(x));      // rows of 16 lanes turned by 4, then by 8
+}
+
+// This lane's part (elements 8*j .. 8*j+7) of row `row` from 16 bytes of bf16.  All 16 lanes of the row take part.
 template <int BITS>
 __device__ inline void write_row(uint8_t* codes, uint8_t* scales, int64_t row, int j, const u32x4& w) {
   uint32_t c[2];
-  const int byte = quantise8<BITS>(w, c);
+  const uint32_t sc = row_scales(quantise8<BITS>(w, c), j);
   uint8_t* dst = codes + row * QFormat<BITS>::kRow + BITS * j;
   if constexpr (BITS == 4) *reinterpret_cast<uint32_t*>(dst) = c[0];
   else *reinterpret_cast<uint64_t*>(dst) = (uint64_t)c[0] | ((uint64_t)c[1] << 32);
-  if ((j & 3) == 0) scales[row * kBlocks + (j >> 2)] = (uint8_t)byte;
+  if (j == 0) *reinterpret_cast<uint32_t*>(scales + row * kBlocks) = sc;
 }
 
 // Rows that sequence s gets.
@@ -143,15 +155,26 @@ __global__ __launch_bounds__(kThreads) void append_q_rows_kernel(QAppendParams p
     const int i0 = (int)(b - pair * per_head) * kGroupRows;
     const int s = (int)(pair / Hkv), g = (int)(pair - (int64_t)s * Hkv);
     const int L = seq_len(p.kv, s), n = new_rows(p, s);
-    for (int i = i0 + threadIdx.x / kRowLanes; i < i0 + kGroupRows; i += kRowsAtOnce) {
+    // every row's loads are issued before the first is used
+    constexpr int kPer = kGroupRows / kRowsAtOnce;
+    u32x4 kw[kPer], vw[kPer];
+    int64_t row[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int i = i0 + threadIdx.x / kRowLanes + u * kRowsAtOnce;
       const int64_t t = (int64_t)L + i;
-      if (i >= n || t >= cap) continue;
-      const int64_t row0 = row_of(p.kv, s, (int)t);
-      if (row0 < 0) continue;
-      const int64_t row = row0 + (int64_t)g * p.kv.stride_head, src = (((int64_t)s * p.n + i) * Hkv + g) * kD + 8 * j;
-      const u32x4 kw = load16(p.k_new + src), vw = load16(p.v_new + src);
-      write_row<BITS>(p.kv.k, p.kv.k_scale, row, j, kw);
-      write_row<BITS>(p.kv.v, p.kv.v_scale, row, j, vw);
+      row[u] = i < n && t < cap ? row_of(p.kv, s, (int)t) : -1;
+      if (row[u] < 0) continue;
+      const int64_t src = (((int64_t)s * p.n + i) * Hkv + g) * kD + 8 * j;
+      kw[u] = load16_nt(p.k_new + src);
+      vw[u] = load16_nt(p.v_new + src);
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      if (row[u] < 0) continue;                            // past the new rows, the capacity or the pool
+      const int64_t at = row[u] + (int64_t)g * p.kv.stride_head;
+      write_row<BITS>(p.kv.k, p.kv.k_scale, at, j, kw[u]);
+      write_row<BITS>(p.kv.v, p.kv.v_scale, at, j, vw[u]);
     }
     if (p.idx) {
       const int m = list_count(p, s);
@@ -186,18 +209,21 @@ __device__ inline u32x4 dequantise8(const uint32_t (&c)[2], int byte) {
   return w;
 }
 
+// This lane's codes and its block's scale byte of a row.
 template <int BITS>
-__device__ inline u32x4 read_row(const uint8_t* codes, const uint8_t* scales, int64_t row, int j) {
+struct Part { uint32_t c[2]; int byte; };
+template <int BITS>
+__device__ inline Part<BITS> read_part(const uint8_t* codes, const uint8_t* scales, int64_t row, int j) {
   const uint8_t* src = codes + row * QFormat<BITS>::kRow + BITS * j;
-  uint32_t c[2] = {0u, 0u};
+  Part<BITS> r{{0u, 0u}, scales[row * kBlocks + (j >> 2)]};
   if constexpr (BITS == 4) {
-    c[0] = *reinterpret_cast<const uint32_t*>(src);
+    r.c[0] = *reinterpret_cast<const uint32_t*>(src);
   } else {
     const uint64_t x = *reinterpret_cast<const uint64_t*>(src);
-    c[0] = (uint32_t)x;
-    c[1] = (uint32_t)(x >> 32);
+    r.c[0] = (uint32_t)x;
+    r.c[1] = (uint32_t)(x >> 32);
   }
-  return dequantise8<BITS>(c, scales[row * kBlocks + (j >> 2)]);
+  return r;
 }
 
 // A workgroup takes kGroupRows output rows of one (sequence, head); rows that the cache does not hold become zero.
@@ -211,18 +237,27 @@ __global__ __launch_bounds__(kThreads) void read_q_kernel(QReadParams p, int64_t
     const int s = (int)(pair / Hkv), g = (int)(pair - (int64_t)s * Hkv);
     const int L = seq_len(p.kv, s);
     const int f = p.first ? p.first[s] : 0;
-    for (int i = i0 + threadIdx.x / kRowLanes; i < i0 + kGroupRows && i < p.n; i += kRowsAtOnce) {
+    // every row's loads are issued before the first is used
+    constexpr int kPer = kGroupRows / kRowsAtOnce;
+    Part<BITS> kp[kPer], vp[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int i = i0 + threadIdx.x / kRowLanes + u * kRowsAtOnce;
       const int64_t t = (int64_t)f + i;
-      int64_t row = t >= 0 && t < L ? row_of(p.kv, s, (int)t) : -1;
-      u32x4 kw = {0u, 0u, 0u, 0u}, vw = {0u, 0u, 0u, 0u};
-      if (row >= 0) {
-        row += (int64_t)g * p.kv.stride_head;
-        if (p.k_out) kw = read_row<BITS>(p.kv.k, p.kv.k_scale, row, j);
-        if (p.v_out) vw = read_row<BITS>(p.kv.v, p.kv.v_scale, row, j);
-      }
+      int64_t row = i < p.n && t >= 0 && t < L ? row_of(p.kv, s, (int)t) : -1;
+      kp[u] = vp[u] = Part<BITS>{{0u, 0u}, QFormat<BITS>::kByteMin};       // zeros
+      if (row < 0) continue;
+      row += (int64_t)g * p.kv.stride_head;
+      if (p.k_out) kp[u] = read_part<BITS>(p.kv.k, p.kv.k_scale, row, j);
+      if (p.v_out) vp[u] = read_part<BITS>(p.kv.v, p.kv.v_scale, row, j);
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int i = i0 + threadIdx.x / kRowLanes + u * kRowsAtOnce;
+      if (i >= p.n) break;
       const int64_t dst = (int64_t)s * p.stride_seq + (int64_t)g * p.stride_head + (int64_t)i * p.stride_tok + 8 * j;
-      if (p.k_out) *reinterpret_cast<u32x4*>(p.k_out + dst) = kw;
-      if (p.v_out) *reinterpret_cast<u32x4*>(p.v_out + dst) = vw;
+      if (p.k_out) store16_nt(p.k_out + dst, dequantise8<BITS>(kp[u].c, kp[u].byte));
+      if (p.v_out) store16_nt(p.v_out + dst, dequantise8<BITS>(vp[u].c, vp[u].byte));
     }
   }
 }
