@@ -465,7 +465,10 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
         }
         return at;
       };
-      // direct loads of tile c into ring slot `slot`
+      // Direct loads of tile c into ring slot `slot`, non-temporal: a call reads each row once, or once a row block and
+      // that at the same time, and the next reader of a layer's cache comes after the other layers'.  Selected rows,
+      // non-temporal and not: 64 heads of 8 bits in pages, 100 and 118 us; 1024 of 4K-8K rows, 32 x 64 heads of 4 bits,
+      // 68 and 78 us; 512 of them 42 and 47 us (where the caches still hold the rows of the call before, 42 and 40).
       auto issue = [&](int c, int slot, const Where& at) {
         const uint32_t dst = ring_lds + (uint32_t)(slot * TL::kBytes);
         if constexpr (ROWS == kQTable) {
@@ -478,8 +481,8 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
               const uint32_t to = dst + 1024u * (uint32_t)(TL::kParts * h + e);
               const uint8_t* kp = p.kv.k + (uint64_t)row_at(16 * h + TL::k_row(lane, e)) * TL::kRow + 16 * TL::k_chunk(lane, e);
               const uint8_t* vp = p.kv.v + (uint64_t)row_at(16 * h + TL::v_row(lane, e)) * TL::kRow + 16 * TL::v_chunk(lane);
-              dma16_hidden(reinterpret_cast<const uint16_t*>(kp), to);
-              dma16_hidden(reinterpret_cast<const uint16_t*>(vp), to + TL::kV);
+              dma16_nt_hidden(reinterpret_cast<const uint16_t*>(kp), to);
+              dma16_nt_hidden(reinterpret_cast<const uint16_t*>(vp), to + TL::kV);
             }
           dma4_hidden((lane < kTile ? p.kv.k_scale : p.kv.v_scale) + (uint64_t)row_at(lane & 31) * kBlocks, dst + TL::kS);
         } else {
@@ -788,7 +791,7 @@ QAttnPlan plan_qattn(int S, int Hkv, int Hq, int nq, int64_t entries, bool gathe
   const int64_t most = kMaxBlocks / pl.n_rb > 1 ? kMaxBlocks / pl.n_rb : 1;
   if (nW > most) nW = most;
   pl.nW = (int)nW;
-  pl.nblk = tiles > INT32_MAX || entries > (1 << 30) || nW * pl.n_rb >= (1 << 22) ? -1 : nW * pl.n_rb;
+  pl.nblk = tiles > (1 << 30) || entries > (1 << 30) || nW * pl.n_rb >= (1 << 22) ? -1 : nW * pl.n_rb;
   pl.counter_bytes = BD_WS_COUNTER_BYTES;
   const size_t rec = sizeof(float) * 16 * pl.nt * (4 + kD);
   pl.record_bytes = nW > 1 && pl.nblk > 0 ? align256(2 * rec * (size_t)pl.nblk) : 0;

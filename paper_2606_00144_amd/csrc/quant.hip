@@ -18,7 +18,10 @@ constexpr int kRowLanes = 16;                  // lanes of a row, 8 elements eac
 constexpr int kRowsAtOnce = kThreads / kRowLanes;
 constexpr int kFusedRows = 16;                 // appends of up to this many rows advance the lengths in the same launch
 constexpr int kFusedThreads = 512;
-constexpr int kGroupRows = 64;                 // rows of one head that a workgroup of the longer calls takes
+// Rows of one head that a workgroup of the longer calls takes.  Written, 32 / 64 / 128 rows: 16K x 8 prompts written
+// and read back in 243 / 243 / 253 us; read back, 16 / 32 / 64 / 128: 16K x 8 in 126 / 115 / 123 / 131 us, in 16-row
+// pages 168 / 147 / 151 / 151.
+constexpr int kWriteRows = 64, kReadRows = 32;
 
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
@@ -145,18 +148,18 @@ __global__ __launch_bounds__(kFusedThreads) void append_q_fused_kernel(QAppendPa
   if (threadIdx.x == 0) advance(p, s, L, n);
 }
 
-// A workgroup takes kGroupRows new rows of one (sequence, head), K and V.
+// A workgroup takes kWriteRows new rows of one (sequence, head), K and V.
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void append_q_rows_kernel(QAppendParams p, int64_t groups, int per_head) {
   const int cap = p.kv.max_seq_len, Hkv = p.kv.num_kv_heads;
   const int j = threadIdx.x % kRowLanes;
   for (int64_t b = blockIdx.x; b < groups; b += gridDim.x) {
     const int64_t pair = b / per_head;
-    const int i0 = (int)(b - pair * per_head) * kGroupRows;
+    const int i0 = (int)(b - pair * per_head) * kWriteRows;
     const int s = (int)(pair / Hkv), g = (int)(pair - (int64_t)s * Hkv);
     const int L = seq_len(p.kv, s), n = new_rows(p, s);
     // every row's loads are issued before the first is used
-    constexpr int kPer = kGroupRows / kRowsAtOnce;
+    constexpr int kPer = kWriteRows / kRowsAtOnce;
     u32x4 kw[kPer], vw[kPer];
     int64_t row[kPer];
 #pragma unroll
@@ -178,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void append_q_rows_kernel(QAppendParams p
     }
     if (p.idx) {
       const int m = list_count(p, s);
-      for (int i = i0 + threadIdx.x; i < i0 + kGroupRows; i += kThreads)
+      for (int i = i0 + threadIdx.x; i < i0 + kWriteRows; i += kThreads)
         if (i < n && L + i < cap && i < p.ld_idx - m) p.idx[((int64_t)s * Hkv + g) * p.ld_idx + m + i] = L + i;
     }
   }
@@ -226,19 +229,19 @@ __device__ inline Part<BITS> read_part(const uint8_t* codes, const uint8_t* scal
   return r;
 }
 
-// A workgroup takes kGroupRows output rows of one (sequence, head); rows that the cache does not hold become zero.
+// A workgroup takes kReadRows output rows of one (sequence, head); rows that the cache does not hold become zero.
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void read_q_kernel(QReadParams p, int64_t groups, int per_head) {
   const int Hkv = p.kv.num_kv_heads;
   const int j = threadIdx.x % kRowLanes;
   for (int64_t b = blockIdx.x; b < groups; b += gridDim.x) {
     const int64_t pair = b / per_head;
-    const int i0 = (int)(b - pair * per_head) * kGroupRows;
+    const int i0 = (int)(b - pair * per_head) * kReadRows;
     const int s = (int)(pair / Hkv), g = (int)(pair - (int64_t)s * Hkv);
     const int L = seq_len(p.kv, s);
     const int f = p.first ? p.first[s] : 0;
     // every row's loads are issued before the first is used
-    constexpr int kPer = kGroupRows / kRowsAtOnce;
+    constexpr int kPer = kReadRows / kRowsAtOnce;
     Part<BITS> kp[kPer], vp[kPer];
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
@@ -273,7 +276,7 @@ hipError_t launch_append_q(const QAppendParams& p, int bits, hipStream_t stream)
     else hipLaunchKernelGGL((append_q_fused_kernel<8>), dim3(S), dim3(kFusedThreads), 0, stream, p);
     return hipGetLastError();
   }
-  const int per_head = (p.n + kGroupRows - 1) / kGroupRows;
+  const int per_head = (p.n + kWriteRows - 1) / kWriteRows;
   const int64_t groups = (int64_t)S * p.kv.num_kv_heads * per_head;
   const dim3 grid((unsigned)(groups < kMaxGrid ? groups : kMaxGrid));
   if (bits == 4) hipLaunchKernelGGL((append_q_rows_kernel<4>), grid, dim3(kThreads), 0, stream, p, groups, per_head);
@@ -285,7 +288,7 @@ hipError_t launch_append_q(const QAppendParams& p, int bits, hipStream_t stream)
 }
 
 hipError_t launch_read_q(const QReadParams& p, int bits, hipStream_t stream) {
-  const int per_head = (p.n + kGroupRows - 1) / kGroupRows;
+  const int per_head = (p.n + kReadRows - 1) / kReadRows;
   const int64_t groups = (int64_t)p.kv.num_seqs * p.kv.num_kv_heads * per_head;
   const dim3 grid((unsigned)(groups < kMaxGrid ? groups : kMaxGrid));
   if (bits == 4) hipLaunchKernelGGL((read_q_kernel<4>), grid, dim3(kThreads), 0, stream, p, groups, per_head);
