@@ -420,7 +420,10 @@ bd_status bd_sample_budgets(const float* u, int32_t count, const int32_t* budget
  *   - 4 scale bytes, one per block of 32 elements (element d: block d / 32).
  * An element's value is its code's value times 2^(scale byte - 127); a block of
  * scale byte 255 is not a number (the microscaling formats MXFP8 and MXFP4).
- * Every value that bd_cache_append_q writes is exact in bf16.
+ * Every value that bd_cache_append_q writes is exact in bf16.  Contents that it
+ * cannot have written (a scale byte outside [16, 254 - emax] other than 255, with
+ * emax 8 for 8 bits and 2 for 4; the e4m3 codes 0x7F and 0xFF) give values that
+ * are not specified.
  *
  * Rows are numbered; row r's codes are at r * (16 * bits) bytes and its scales
  * at 4 * r bytes of their arrays, in K and V alike.  Strides count rows:
@@ -429,7 +432,8 @@ bd_status bd_sample_budgets(const float* u, int32_t count, const int32_t* budget
  *   + g*stride_head + (t % page_size)*stride_tok.
  * Page numbers, lengths and the causal rule are those of bd_kv_desc.  Page
  * sizes that are multiples of 16 are read through one table entry per page.
- * Limits (BD_ERR_UNSUPPORTED beyond): 2^31 - 1 rows, stride_tok of 2^19 rows. */
+ * Limits (BD_ERR_UNSUPPORTED beyond): 2^31 - 1 rows, max_seq_len of 2^30,
+ * stride_tok of 2^19 rows. */
 typedef struct bd_qkv_desc {
   uint8_t* k;                 /* codes, 16-byte aligned; only bd_cache_append_q writes */
   uint8_t* v;
@@ -484,7 +488,8 @@ bd_status bd_cache_append_q(const bd_qkv_desc* kv, const uint16_t* k_new, const 
  * first      NULL (0), or device [S].
  * k_out, v_out  bf16, element (s, g, i, d) at s*out_stride_seq + g*out_stride_head
  *            + i*out_stride_tok + d; 16-byte aligned; either may be NULL.  Strides
- *            are non-negative multiples of 8 elements.  n up to 2^30.
+ *            are non-negative multiples of 8 elements; rows must not overlap.  n up
+ *            to 2^30.
  * ---------------------------------------------------------------------- */
 bd_status bd_cache_read_q(const bd_qkv_desc* kv, const int32_t* first, int32_t n, uint16_t* k_out, uint16_t* v_out,
                           int64_t out_stride_seq, int64_t out_stride_head, int64_t out_stride_tok, hipStream_t stream);

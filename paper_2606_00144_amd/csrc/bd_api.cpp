@@ -662,6 +662,7 @@ bd_status check_qkv(const bd_qkv_desc* kv, bool need_k, bool need_v, int32_t num
                 kv->num_kv_heads);
   if ((int64_t)kv->num_seqs * kv->num_kv_heads > kMaxPairs || num_q_heads / kv->num_kv_heads > kMaxGroup)
     return fail(BD_ERR_UNSUPPORTED, "more than 2^24 (sequence, KV head) pairs or 2^16 query heads per KV head");
+  if (kv->max_seq_len > (1 << 30)) return fail(BD_ERR_UNSUPPORTED, "max_seq_len above 2^30");   // lengths + 2^30 rows fit
   const int64_t far = (int64_t)1 << 31;                       // no stride of a layout of fewer rows is larger
   if (kv->stride_head < 0 || kv->stride_tok < 0 || (kv->page_table ? kv->stride_page : kv->stride_seq) < 0)
     return fail(BD_ERR_INVALID_ARG, "strides must not be negative");

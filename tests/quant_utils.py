@@ -5,7 +5,7 @@ import torch
 import oracle as O
 import paper_2606_00144_amd as bd
 import synth
-from gpu_utils import bf16_dev, bf16_host64, i32_dev
+from gpu_utils import bf16_host64
 
 
 def bits_of(x):

@@ -10,7 +10,7 @@ import torch
 import oracle as O
 import paper_2606_00144_amd as bd
 from gpu_utils import bf16_dev, bf16_host64, case, i32_dev, poison_workspace
-from quant_utils import (bits_of, check_out, garbage, make_cache, rows, special_rows, to_dev, to_host, to_pages,
+from quant_utils import (check_out, garbage, make_cache, rows, special_rows, to_dev, to_host, to_pages,
                          values_as_bits)
 
 pytestmark = pytest.mark.gpu
@@ -446,6 +446,108 @@ def test_graphs_replayed_side_by_side():
             want = bd.bd_verify_attn_q(dev, q, i32_dev(n))
             torch.cuda.synchronize()
             assert torch.equal(o.view(torch.int16), want.view(torch.int16)), r
+
+
+@BITS
+def test_sequences_that_share_pages(bits):
+    # a common prefix kept once: every sequence's table begins with the same pages
+    S, Hq, Hkv, L, gamma, page = 4, 8, 2, 320, 3, 16
+    lens = [320, 257, 300, 100]
+    cache, kb, vb = make_cache(1, Hkv, L, bits, [L], 180)
+    pool, table = to_pages(cache, [L], page, 181)
+    kb, vb = np.repeat(kb, S, 0), np.repeat(vb, S, 0)
+    q = rows((S, gamma + 1, Hq, 128), 182)
+    kw = dict(page_table=i32_dev(np.repeat(table, S, 0)), max_seq_len=L)
+    case(f"shared pages bits={bits}")
+    dev = to_dev(pool)
+    out, lse = bd.bd_verify_attn_q(dev, bf16_dev(q), i32_dev(lens), return_lse=True, **kw)
+    k, v = bd.bd_cache_read_q(dev, i32_dev(lens), L, **kw)
+    torch.cuda.synchronize()
+    ref = lambda q, k, v: O.verify_attn(k, v, q, lens, gamma)
+    check_out(out, lse, *ref(q, kb, vb), kb, vb, q, ref, L, "shared pages")
+    for s, n in enumerate(lens):
+        assert np.array_equal(_u16(k)[s, :, :n], kb[s, :, :n]) and np.array_equal(_u16(v)[s, :, :n], vb[s, :, :n])
+        assert not _u16(k)[s, :, n:].any() and not _u16(v)[s, :, n:].any()
+
+
+def test_calls_on_two_streams():
+    # default scratch is a stream's own: calls that overlap give what they give alone
+    S, L = 2, 9000
+    cache, kb, vb = make_cache(S, 2, L, 4, [L, L], 190)
+    dev, lens = to_dev(cache), [i32_dev([9000, 4000]), i32_dev([33, 8000])]
+    qs = [bf16_dev(rows((S, 6, 8, 128), 191 + i)) for i in range(2)]
+    idx = i32_dev(np.random.default_rng(3).integers(0, L, (S, 2, 700)).astype(np.int32))
+    nsel = i32_dev([700, 650])
+    both = lambda i: (bd.bd_verify_attn_q(dev, qs[i], lens[i]),
+                      bd.bd_sparse_decode_attn_q(dev, qs[i][:, 0].contiguous(), idx, nsel, lens[i]))
+    case("two streams")
+    want = [both(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        got = [[], []]
+        for _ in range(4):
+            for i, st in enumerate(streams):
+                with torch.cuda.stream(st):
+                    got[i].append(both(i))
+        torch.cuda.synchronize()
+        for i in range(2):
+            for a in got[i]:
+                assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(a, want[i]))
+
+
+@BITS
+def test_a_round_captured_and_replayed(bits):
+    # append, draft, verification and rollback in one graph; each replay grows the caches as the eager round does
+    S, Hq, Hkv, cap, L0, gamma = 2, 8, 2, 600, [130, 401], 3
+    cache, kb, vb = make_cache(S, Hkv, cap, bits, L0, 200)
+    kn, vn = bf16_dev(rows((S, gamma + 1, Hkv, 128), 201)), bf16_dev(rows((S, gamma + 1, Hkv, 128), 202))
+    q = bf16_dev(rows((S, gamma + 1, Hq, 128), 203))
+    acc = i32_dev([1, 3])
+
+    class State:
+        def __init__(self):
+            self.dev, self.lens = to_dev(cache), i32_dev(L0)
+            self.idx = torch.full((S, Hkv, 100), -1, dtype=torch.int32, device="cuda")
+            self.idx[:, :, :60] = torch.arange(60, dtype=torch.int32, device="cuda")
+            self.nsel = i32_dev([60, 60])
+            self.base_l, self.base_n = self.lens.clone(), self.nsel.clone()
+            self.draft, self.ver = torch.empty((S, Hq, 128), dtype=torch.bfloat16, device="cuda"), torch.empty_like(q)
+            self.q0 = q[:, 0].contiguous()
+            self.read = tuple(torch.empty((S, Hkv, 7, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            self.ws = bd.Workspace()
+
+        def round(self):
+            self.base_l.copy_(self.lens)
+            self.base_n.copy_(self.nsel)
+            bd.bd_cache_append_q(self.dev, self.lens, kn, vn, idx=self.idx, nsel=self.nsel)
+            bd.bd_sparse_decode_attn_q(self.dev, self.q0, self.idx, self.nsel, self.lens, out=self.draft, workspace=self.ws)
+            bd.bd_verify_attn_q(self.dev, q, self.lens, out=self.ver, workspace=self.ws)
+            bd.bd_cache_read_q(self.dev, self.lens, 7, first=self.base_l, outputs=self.read)
+            bd.bd_cache_rollback(self.lens, acc, gamma + 1, nsel=self.nsel, base_lens=self.base_l, base_nsel=self.base_n)
+
+        def bytes(self):
+            return [t.view(torch.uint8) for t in (*self.dev, self.lens, self.idx, self.nsel, self.draft, self.ver, *self.read)]
+
+    case(f"captured round bits={bits}")
+    eager, captured = State(), State()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured.round()                                     # sizes the workspace
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured.round()
+    eager.round()
+    for _ in range(4):
+        g.replay()
+        torch.cuda.synchronize()
+        eager.round()
+        torch.cuda.synchronize()
+        for a, b in zip(captured.bytes(), eager.bytes()):
+            assert torch.equal(a, b)
 
 
 @BITS

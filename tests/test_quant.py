@@ -9,7 +9,7 @@ import torch
 
 import oracle as O
 import paper_2606_00144_amd as bd
-from quant_utils import bits_of, rows, special_rows, values_as_bits
+from quant_utils import bits_of, rows, special_rows
 
 FAKE = 0x10000000
 BITS = pytest.mark.parametrize("bits", [4, 8])
@@ -229,7 +229,7 @@ def test_shared_rejections(L):
     inv, uns = bd.BD_ERR_INVALID_ARG, bd.BD_ERR_UNSUPPORTED
     cases = [(dict(head_dim=64), uns), (dict(bits=6), uns), (dict(k=0), inv), (dict(v_scale=0), inv), (dict(k=FAKE + 8), inv),
              (dict(k_scale=FAKE + 2), inv), (dict(seq_lens=0), inv), (dict(num_seqs=0), inv), (dict(num_kv_heads=0), inv),
-             (dict(max_seq_len=-1), inv), (dict(stride_tok=-1), inv), (dict(stride_seq=-8), inv),
+             (dict(max_seq_len=-1), inv), (dict(max_seq_len=(1 << 30) + 1, stride_tok=0), uns), (dict(stride_tok=-1), inv), (dict(stride_seq=-8), inv),
              (dict(stride_tok=(1 << 19) + 1), uns), (dict(stride_head=1 << 31), uns), (dict(stride_seq=1 << 40), uns),
              (dict(num_seqs=2 ** 21, num_kv_heads=16), uns), (dict(stride_seq=(1 << 31) - 1, stride_head=1), uns),
              (dict(PAGED, page_size=0), inv), (dict(PAGED, num_pages=0), inv), (dict(PAGED, max_pages_per_seq=255), inv),
