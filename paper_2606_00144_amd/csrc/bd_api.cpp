@@ -712,7 +712,6 @@ bd_status run_qattn(const bd_qkv_desc* kv, const uint16_t* q, int32_t Hq, int32_
   p.R = pl.R;
   p.n_rb = pl.n_rb;
   p.nW = pl.nW;
-  p.min_share = pl.min_share;
   p.scale_log2 = scale * 1.4426950408889634f;
   p.counters = static_cast<uint32_t*>(ws);
   p.part = pl.record_bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + pl.counter_bytes) : nullptr;

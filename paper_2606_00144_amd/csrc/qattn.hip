@@ -36,6 +36,11 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kTile = 32;                      // keys per wave step
 constexpr int kGroup = 8;                      // records merged by one workgroup at a time
+// Shares are at least kMinSpan tiles long, a unit counts as that many even if it has fewer (its prologue and merge take
+// the time of about that many), and a unit of fewer than kWhole tiles is not cut: the share that has the larger part
+// of it takes it.  Shares of at least 4 / 8 / 16 / 24 tiles: 8 heads of one 8K sequence 14.9 / 13.5 / 15.4 / 20.6 us,
+// one 4K decode of 2 heads 10.1 / 9.2 / 11.5 / 11.5.
+constexpr int kMinSpan = 8, kWhole = 16;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                  // lazy-rescale headroom, log2 units
 constexpr uint32_t kAbsent = 0xFFFFFFFFu;
@@ -275,8 +280,9 @@ __device__ inline int unit_keys(const QAttnParams& p, int s, int& L) {
   const int n = p.nsel[s];
   return n < 0 || L == 0 ? 0 : (n > p.ld_idx ? p.ld_idx : n);   // an empty cache has no row to stand in for absent ones
 }
-// Tiles of a unit: an empty one still takes part, its outputs have to be written.
+// Tiles of a unit (an empty one has one too: its outputs have to be written), and its length in the stream.
 __device__ inline int unit_tiles(int n) { return n > 0 ? (int)(((int64_t)n + kTile - 1) / kTile) : 1; }
+__device__ inline int unit_span(int n) { const int t = unit_tiles(n); return t > kMinSpan ? t : kMinSpan; }
 
 // Inclusive sums over the lanes.
 template <int CTRL, int ROWMASK>
@@ -301,7 +307,7 @@ __device__ inline int fetch_args(const QAttnParams& p) {
   asm("s_mov_b32 %0, 0" : "=s"(z1) : "s"(z0), "s"(p.kv.stride_page), "s"(p.kv.max_seq_len), "s"(p.kv.page_size),
       "s"(p.kv.max_pages_per_seq), "s"(p.kv.num_pages), "s"(p.q), "s"(p.out), "s"(p.lse), "s"(p.idx), "s"(p.nsel));
   asm("s_mov_b32 %0, 0" : "=s"(z2) : "s"(z1), "s"(p.ld_idx), "s"(p.S), "s"(p.Hkv), "s"(p.Hq), "s"(p.G), "s"(p.nq),
-      "s"(p.R), "s"(p.n_rb), "s"(p.nW), "s"(p.min_share), "s"(p.scale_log2), "s"(p.part), "s"(p.part_bytes),
+      "s"(p.R), "s"(p.n_rb), "s"(p.nW), "s"(p.scale_log2), "s"(p.part), "s"(p.part_bytes),
       "s"(p.counters));
   return z2;
 }
@@ -320,31 +326,31 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
   const int share = bid / p.n_rb, rb = bid - share * p.n_rb;
   const bool gather = p.idx != nullptr;
 
-  // ---- the share: tiles [pos, end) of the stream, the first of them in sequence s
+  // ---- the share: tiles [begin, end) of the stream, the first of them in sequence s
   int total = 0, first_w = 0;                  // first_w: this lane's sequence of the first 64, in tiles
   for (int s0 = 0; s0 < p.S; s0 += kWave) {
     int L = 0, w = 0;
-    if (s0 + lane < p.S) w = unit_tiles(unit_keys(p, s0 + lane, L)) * p.Hkv;
+    if (s0 + lane < p.S) w = unit_span(unit_keys(p, s0 + lane, L)) * p.Hkv;
     w = wave_scan(w);
     if (s0 == 0) first_w = w;
     total += __builtin_amdgcn_readlane(w, kWave - 1);
   }
   int chunk = (total + p.nW - 1) / p.nW;
-  if (chunk < p.min_share) chunk = p.min_share;
-  const int64_t pos64 = (int64_t)share * chunk;
-  if (pos64 >= total) return;
-  int pos = (int)pos64;
-  const int end = total - pos < chunk ? total : pos + chunk;
+  if (chunk < kMinSpan) chunk = kMinSpan;
+  const int64_t begin64 = (int64_t)share * chunk;
+  if (begin64 >= total) return;
+  const int begin = (int)begin64;
+  const int end = total - begin < chunk ? total : begin + chunk;
   int s = 0, before = 0;                       // tiles of the sequences before s
   for (int s0 = 0, acc = 0; s0 < p.S; s0 += kWave) {
     int w = first_w;
     if (s0 > 0) {
       int L = 0;
       w = 0;
-      if (s0 + lane < p.S) w = unit_tiles(unit_keys(p, s0 + lane, L)) * p.Hkv;
+      if (s0 + lane < p.S) w = unit_span(unit_keys(p, s0 + lane, L)) * p.Hkv;
       w = wave_scan(w);
     }
-    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(acc + w <= pos));
+    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(acc + w <= begin));
     if (c < kWave) {
       s = s0 + c;
       before = acc + (c > 0 ? __builtin_amdgcn_readlane(w, c - 1) : 0);
@@ -357,9 +363,9 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
 
   int L, n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
   L = __builtin_amdgcn_readfirstlane(L);
-  int T = unit_tiles(n);
-  int g = (pos - before) / T;
-  int unit0 = before + g * T;                  // the unit's first tile in the stream
+  int T = unit_tiles(n), span = unit_span(n);
+  int g = (begin - before) / span;
+  int unit0 = before + g * span;               // the unit's first tile in the stream
 
   const uint32_t ring_lds = lds_addr(&sm.u.ring[wave][0][0]);
   const uint32_t tok = (uint32_t)p.kv.stride_tok, tok_bytes = tok * (uint32_t)TL::kRow;   // 15 rows below 2^31: host-checked
@@ -370,9 +376,29 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
     v_off[e] = (uint32_t)TL::v_row(lane, e) * tok_bytes + 16u * (uint32_t)TL::v_chunk(lane);
   }
 
+  // whether the share has a piece of the unit
+  auto taken = [&] { return T >= kWhole || (begin - unit0 < (span + 1) / 2 && end - unit0 >= (span + 1) / 2); };
+  // to the next unit; false where the share ends
+  auto advance = [&] {
+    unit0 += span;
+    if (unit0 >= end) return false;
+    if (++g == p.Hkv) {
+      g = 0;
+      ++s;
+      n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
+      L = __builtin_amdgcn_readfirstlane(L);
+      T = unit_tiles(n);
+      span = unit_span(n);
+    }
+    return true;
+  };
+  while (!taken())
+    if (!advance()) return;
+
   for (;;) {   // ---- one piece: tiles [t0, t1) of unit (s, g)
-    const int t0 = pos - unit0;
-    const int t1 = T - t0 < end - pos ? T : t0 + (end - pos);
+    const bool whole = T < kWhole;
+    const int t0 = whole || begin <= unit0 ? 0 : begin - unit0;
+    const int t1 = whole || T <= end - unit0 ? T : end - unit0;
     const int tn = (n + kTile - 1) / kTile < t1 ? (n + kTile - 1) / kTile : t1;   // tiles that hold keys
 
     const int lane_q = here(lane), lgq = lane_q >> 4, lrq = lane_q & 15;
@@ -651,7 +677,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
 
     // ---- pieces of the unit: shares w0 .. w1
     const int w0 = unit0 / chunk, w1 = (unit0 + T - 1) / chunk;
-    if (w0 == w1) {
+    if (whole || w0 == w1) {
       write_final(M, Ls, Lx, acc);
     } else {
       const __amdgpu_buffer_rsrc_t rec = make_rsrc(p.part, p.part_bytes);
@@ -746,17 +772,9 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       }
     }
 
-    pos += t1 - t0;
-    if (pos >= end) break;
-    // the share goes on: the next unit from its first tile
-    unit0 += T;
-    if (++g == p.Hkv) {
-      g = 0;
-      ++s;
-      n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
-      L = __builtin_amdgcn_readfirstlane(L);
-      T = unit_tiles(n);
-    }
+    do {
+      if (!advance()) return;
+    } while (!taken());
     __syncthreads();   // the merge buffer is read: the ring may be filled again
   }
 }
@@ -785,9 +803,9 @@ QAttnPlan plan_qattn(int S, int Hkv, int Hq, int nq, int64_t entries, bool gathe
   pl.nt = R <= 16 ? 1 : 2;
   pl.n_rb = (pl.R + 16 * pl.nt - 1) / (16 * pl.nt);
   pl.rows = gather ? kQTable : !paged ? kQContiguous : page_size % 16 == 0 ? kQPages : kQTable;
-  pl.min_share = 8;
-  const int64_t tiles = (int64_t)S * Hkv * (entries > 0 ? (entries + kTile - 1) / kTile : 1);
-  int64_t nW = (tiles + pl.min_share - 1) / pl.min_share;
+  const int64_t span = (entries + kTile - 1) / kTile;
+  const int64_t tiles = (int64_t)S * Hkv * (span > kMinSpan ? span : kMinSpan);
+  int64_t nW = (tiles + kMinSpan - 1) / kMinSpan;
   const int64_t most = kMaxBlocks / pl.n_rb > 1 ? kMaxBlocks / pl.n_rb : 1;
   if (nW > most) nW = most;
   pl.nW = (int)nW;

@@ -99,7 +99,6 @@ struct QAttnParams {
   int32_t R;                // rows per (s, g): nq * G
   int32_t n_rb;             // row blocks
   int32_t nW;               // shares of the key stream
-  int32_t min_share;        // tiles that a share holds at least
   float scale_log2;         // softmax scale * log2(e)
   float* part;              // partial records: two per workgroup
   uint32_t part_bytes;
@@ -107,7 +106,7 @@ struct QAttnParams {
 };
 
 struct QAttnPlan {
-  int nt, n_rb, R, nW, min_share;
+  int nt, n_rb, R, nW;
   QRows rows;
   int64_t nblk;             // workgroups, -1: too many
   size_t counter_bytes, record_bytes, ws_bytes;
