@@ -284,6 +284,13 @@ __device__ inline int unit_keys(const QAttnParams& p, int s, int& L) {
 __device__ inline int unit_tiles(int n) { return n > 0 ? (int)(((int64_t)n + kTile - 1) / kTile) : 1; }
 __device__ inline int unit_span(int n) { const int t = unit_tiles(n); return t > kMinSpan ? t : kMinSpan; }
 
+// Shares that a unit of t tiles has of its own (t = 0: no unit), of about c tiles each.  Whatever the rounding of the
+// products gives lies in [1, t], and is the same in every workgroup.
+__device__ inline int own_shares(int t, int c) {
+  const int k = (int)(((float)t - 0.5f) * __builtin_amdgcn_rcpf((float)c)) + 1;
+  return t < kWhole ? (t > 0 ? 1 : 0) : k;
+}
+
 // Inclusive sums over the lanes.
 template <int CTRL, int ROWMASK>
 __device__ inline int add_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWMASK, 0xF, false); }
@@ -326,17 +333,44 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
   const int share = bid / p.n_rb, rb = bid - share * p.n_rb;
   const bool gather = p.idx != nullptr;
 
-  // ---- the share: tiles [begin, end) of the stream, the first of them in sequence s
-  int total = 0, first_w = 0;                  // first_w: this lane's sequence of the first 64, in tiles
+  // ---- the share: [begin, end) of the stream, its first piece in sequence s.  The stream is counted in tiles and cut
+  // every `chunk` of them; or, with per > 0, each unit has shares of its own, of `per` tiles or a little less, and the
+  // stream is counted in shares.  So it is where such shares are at most 9 tiles longer: a share that has parts of two
+  // units does two prologues and two merges one after the other (22 sequences of 650 to 2602 rows, 8 heads, 28 rows,
+  // 4 bits: 25.2 -> 19.3 us; 27 of 816 to 3267, 4 heads, 24 rows, 8 bits: 28.4 -> 22.6).
+  int total = 0, first_w = 0, first_t = 0;     // of this lane's sequence of the first 64: its end, its units' tiles
   for (int s0 = 0; s0 < p.S; s0 += kWave) {
     int L = 0, w = 0;
-    if (s0 + lane < p.S) w = unit_span(unit_keys(p, s0 + lane, L)) * p.Hkv;
+    if (s0 + lane < p.S) {
+      const int n = unit_keys(p, s0 + lane, L);
+      w = unit_span(n) * p.Hkv;
+      if (s0 == 0) first_t = unit_tiles(n);
+    }
     w = wave_scan(w);
     if (s0 == 0) first_w = w;
     total += __builtin_amdgcn_readlane(w, kWave - 1);
   }
   int chunk = (total + p.nW - 1) / p.nW;
   if (chunk < kMinSpan) chunk = kMinSpan;
+  int per = 0;
+  if (p.S <= kWave && p.S * p.Hkv <= p.nW) {
+    // the shares that four lengths give, two sums to a word (below 2 nW each: a unit has at most one more than its part)
+    const int shares0 = (own_shares(first_t, chunk) | own_shares(first_t, chunk + 2) << 16) * p.Hkv;
+    const int shares1 = (own_shares(first_t, chunk + 5) | own_shares(first_t, chunk + 9) << 16) * p.Hkv;
+    const int ends0 = wave_scan(shares0), ends1 = wave_scan(shares1);
+    const uint32_t sum0 = (uint32_t)__builtin_amdgcn_readlane(ends0, kWave - 1), sum1 = (uint32_t)__builtin_amdgcn_readlane(ends1, kWave - 1);
+    const uint32_t nW = (uint32_t)p.nW;
+    if ((sum1 >> 16) <= nW) {
+      const bool low = (sum0 & 0xFFFFu) <= nW || ((sum0 >> 16) > nW && (sum1 & 0xFFFFu) <= nW);
+      const bool first = (sum0 & 0xFFFFu) <= nW || (sum0 >> 16) <= nW;
+      per = chunk + (first ? (low ? 0 : 2) : (low ? 5 : 9));
+      const uint32_t e = first ? (uint32_t)ends0 : (uint32_t)ends1, t = first ? sum0 : sum1;
+      first_w = (int)(low ? e & 0xFFFFu : e >> 16);
+      total = (int)(low ? t & 0xFFFFu : t >> 16);
+      chunk = 1;
+    }
+  }
+  auto span_of = [&](int n) { return per == 0 ? unit_span(n) : own_shares(unit_tiles(n), per); };
   const int64_t begin64 = (int64_t)share * chunk;
   if (begin64 >= total) return;
   const int begin = (int)begin64;
@@ -363,9 +397,9 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
 
   int L, n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
   L = __builtin_amdgcn_readfirstlane(L);
-  int T = unit_tiles(n), span = unit_span(n);
+  int T = unit_tiles(n), span = span_of(n);
   int g = (begin - before) / span;
-  int unit0 = before + g * span;               // the unit's first tile in the stream
+  int unit0 = before + g * span;               // where the unit begins in the stream
 
   const uint32_t ring_lds = lds_addr(&sm.u.ring[wave][0][0]);
   const uint32_t tok = (uint32_t)p.kv.stride_tok, tok_bytes = tok * (uint32_t)TL::kRow;   // 15 rows below 2^31: host-checked
@@ -377,7 +411,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
   }
 
   // whether the share has a piece of the unit
-  auto taken = [&] { return T >= kWhole || (begin - unit0 < (span + 1) / 2 && end - unit0 >= (span + 1) / 2); };
+  auto taken = [&] { return per > 0 || T >= kWhole || (begin - unit0 < (span + 1) / 2 && end - unit0 >= (span + 1) / 2); };
   // to the next unit; false where the share ends
   auto advance = [&] {
     unit0 += span;
@@ -388,7 +422,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
       L = __builtin_amdgcn_readfirstlane(L);
       T = unit_tiles(n);
-      span = unit_span(n);
+      span = span_of(n);
     }
     return true;
   };
@@ -397,8 +431,13 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
 
   for (;;) {   // ---- one piece: tiles [t0, t1) of unit (s, g)
     const bool whole = T < kWhole;
-    const int t0 = whole || begin <= unit0 ? 0 : begin - unit0;
-    const int t1 = whole || T <= end - unit0 ? T : end - unit0;
+    int t0 = whole || begin <= unit0 ? 0 : begin - unit0;
+    int t1 = whole || T <= end - unit0 ? T : end - unit0;
+    if (per > 0 && !whole) {   // the share's part of T tiles, cut evenly
+      const int j = begin - unit0, q = T / span, more = T - q * span;
+      t0 = j * q + (j < more ? j : more);
+      t1 = t0 + q + (j < more ? 1 : 0);
+    }
     const int tn = (n + kTile - 1) / kTile < t1 ? (n + kTile - 1) / kTile : t1;   // tiles that hold keys
 
     const int lane_q = here(lane), lgq = lane_q >> 4, lrq = lane_q & 15;
@@ -676,7 +715,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
     };
 
     // ---- pieces of the unit: shares w0 .. w1
-    const int w0 = unit0 / chunk, w1 = (unit0 + T - 1) / chunk;
+    const int w0 = unit0 / chunk, w1 = (unit0 + span - 1) / chunk;
     if (whole || w0 == w1) {
       write_final(M, Ls, Lx, acc);
     } else {
@@ -805,7 +844,7 @@ QAttnPlan plan_qattn(int S, int Hkv, int Hq, int nq, int64_t entries, bool gathe
   pl.rows = gather ? kQTable : !paged ? kQContiguous : page_size % 16 == 0 ? kQPages : kQTable;
   const int64_t span = (entries + kTile - 1) / kTile;
   const int64_t tiles = (int64_t)S * Hkv * (span > kMinSpan ? span : kMinSpan);
-  int64_t nW = (tiles + kMinSpan - 1) / kMinSpan;
+  int64_t nW = (int64_t)S * Hkv * (((span > kMinSpan ? span : kMinSpan) + kMinSpan - 1) / kMinSpan);   // whole shares a unit
   const int64_t most = kMaxBlocks / pl.n_rb > 1 ? kMaxBlocks / pl.n_rb : 1;
   if (nW > most) nW = most;
   pl.nW = (int)nW;

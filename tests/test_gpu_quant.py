@@ -215,6 +215,16 @@ def test_verify_many_sequences(bits, S):
     _verify(S, 4, 2, 400, lens, 2, bits, S, "many sequences")
 
 
+@BITS
+@pytest.mark.parametrize("S,Hkv,top", [(24, 4, 2600), (9, 8, 900), (60, 2, 700), (3, 2, 5000), (40, 4, 300)])
+def test_verify_ragged_batches(bits, S, Hkv, top):
+    # units with shares of their own of every length, shares of two units, short units that are not cut
+    r = np.random.default_rng(S + bits)
+    lens = np.exp(r.uniform(np.log(20), np.log(top), S)).astype(int).tolist()
+    lens[0], lens[1] = top, 0
+    _verify(S, 2 * Hkv, Hkv, top, lens, 4, bits, S, "ragged", page=16 if S % 2 else 0)
+
+
 @pytest.mark.parametrize("bits,L,Hkv,page", [(4, 20000, 1, 0), (8, 20000, 1, 16), (4, 9000, 3, 0), (4, 70000, 1, 16), (8, 5000, 1, 24)])
 def test_verify_one_long_sequence(bits, L, Hkv, page):
     # units of many pieces: the two-level merge; tables filled more than once
