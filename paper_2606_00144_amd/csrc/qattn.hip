@@ -40,7 +40,7 @@ constexpr int kGroup = 8;                      // records merged by one workgrou
 // the time of about that many), and a unit of fewer than kWhole tiles is not cut: the share that has the larger part
 // of it takes it.  Shares of at least 4 / 8 / 16 / 24 tiles: 8 heads of one 8K sequence 14.9 / 13.5 / 15.4 / 20.6 us,
 // one 4K decode of 2 heads 10.1 / 9.2 / 11.5 / 11.5.
-constexpr int kMinSpan = 8, kWhole = 16;
+constexpr int kMinSpan = 8, kWhole = 16, kLonger = 6;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;                  // lazy-rescale headroom, log2 units
 constexpr uint32_t kAbsent = 0xFFFFFFFFu;
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
 
   // ---- the share: [begin, end) of the stream, its first piece in sequence s.  The stream is counted in tiles and cut
   // every `chunk` of them; or, with per > 0, each unit has shares of its own, of `per` tiles or a little less, and the
-  // stream is counted in shares.  So it is where such shares are at most 9 tiles longer: a share that has parts of two
+  // stream is counted in shares.  So it is where such shares are no more than kLonger tiles longer: a share that has parts of two
   // units does two prologues and two merges one after the other (22 sequences of 650 to 2602 rows, 8 heads, 28 rows,
   // 4 bits: 25.2 -> 19.3 us; 27 of 816 to 3267, 4 heads, 24 rows, 8 bits: 28.4 -> 22.6).
   int total = 0, first_w = 0, first_t = 0;     // of this lane's sequence of the first 64: its end, its units' tiles
@@ -354,23 +354,17 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
   if (chunk < kMinSpan) chunk = kMinSpan;
   int per = 0;
   if (p.S <= kWave && p.S * p.Hkv <= p.nW) {
-    // the shares that four lengths give, two sums to a word (below 2 nW each: a unit has at most one more than its part)
-    const int shares0 = (own_shares(first_t, chunk) | own_shares(first_t, chunk + 2) << 16) * p.Hkv;
-    const int shares1 = (own_shares(first_t, chunk + 5) | own_shares(first_t, chunk + 9) << 16) * p.Hkv;
-    const int ends0 = wave_scan(shares0), ends1 = wave_scan(shares1);
-    const uint32_t sum0 = (uint32_t)__builtin_amdgcn_readlane(ends0, kWave - 1), sum1 = (uint32_t)__builtin_amdgcn_readlane(ends1, kWave - 1);
-    const uint32_t nW = (uint32_t)p.nW;
-    if ((sum1 >> 16) <= nW) {
-      const bool low = (sum0 & 0xFFFFu) <= nW || ((sum0 >> 16) > nW && (sum1 & 0xFFFFu) <= nW);
-      const bool first = (sum0 & 0xFFFFu) <= nW || (sum0 >> 16) <= nW;
-      per = chunk + (first ? (low ? 0 : 2) : (low ? 5 : 9));
-      const uint32_t e = first ? (uint32_t)ends0 : (uint32_t)ends1, t = first ? sum0 : sum1;
-      first_w = (int)(low ? e & 0xFFFFu : e >> 16);
-      total = (int)(low ? t & 0xFFFFu : t >> 16);
+    // the shares that two lengths give, in one word (sums below 2 nW: a unit has at most one more than its part)
+    const int ends = wave_scan((own_shares(first_t, chunk) | own_shares(first_t, chunk + kLonger) << 16) * p.Hkv);
+    const uint32_t sums = (uint32_t)__builtin_amdgcn_readlane(ends, kWave - 1);
+    const int part = (sums & 0xFFFFu) <= (uint32_t)p.nW ? 0 : 16;
+    if ((sums >> part & 0xFFFFu) <= (uint32_t)p.nW) {
+      per = part ? chunk + kLonger : chunk;
+      first_w = (int)((uint32_t)ends >> part & 0xFFFFu);
+      total = (int)(sums >> part & 0xFFFFu);
       chunk = 1;
     }
   }
-  auto span_of = [&](int n) { return per == 0 ? unit_span(n) : own_shares(unit_tiles(n), per); };
   const int64_t begin64 = (int64_t)share * chunk;
   if (begin64 >= total) return;
   const int begin = (int)begin64;
@@ -397,7 +391,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
 
   int L, n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
   L = __builtin_amdgcn_readfirstlane(L);
-  int T = unit_tiles(n), span = span_of(n);
+  int T = unit_tiles(n), span = per == 0 ? unit_span(n) : own_shares(T, per);
   int g = (begin - before) / span;
   int unit0 = before + g * span;               // where the unit begins in the stream
 
@@ -412,7 +406,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
 
   // whether the share has a piece of the unit
   auto taken = [&] { return per > 0 || T >= kWhole || (begin - unit0 < (span + 1) / 2 && end - unit0 >= (span + 1) / 2); };
-  // to the next unit; false where the share ends
+  // to the next unit; false where the share ends (with per > 0 it always does)
   auto advance = [&] {
     unit0 += span;
     if (unit0 >= end) return false;
@@ -422,7 +416,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       n = __builtin_amdgcn_readfirstlane(unit_keys(p, s, L));
       L = __builtin_amdgcn_readfirstlane(L);
       T = unit_tiles(n);
-      span = span_of(n);
+      span = unit_span(n);
     }
     return true;
   };
