@@ -790,9 +790,11 @@ bd_status bd_sparse_decode_attn_q(const bd_qkv_desc* kv, const uint16_t* q, int3
 size_t bd_verify_attn_q_workspace_bytes(int32_t num_seqs, int32_t num_kv_heads, int32_t num_q_heads, int32_t gamma,
                                         int32_t max_seq_len) {
   if (!shape_ok(num_seqs, num_kv_heads, num_q_heads) || gamma < 0 || gamma > 4095 || max_seq_len < 0) return 0;
-  // the same for every layout
+  // the larger of the layouts': contiguous or pages of whole 16-row parts, and other pages
   const bd::QAttnPlan pl = bd::plan_qattn(num_seqs, num_kv_heads, num_q_heads, gamma + 1, max_seq_len, false, false, 0);
-  return pl.nblk < 0 ? 0 : pl.ws_bytes;
+  const bd::QAttnPlan odd = bd::plan_qattn(num_seqs, num_kv_heads, num_q_heads, gamma + 1, max_seq_len, false, true, 1);
+  const size_t a = pl.nblk < 0 ? 0 : pl.ws_bytes, b = odd.nblk < 0 ? 0 : odd.ws_bytes;
+  return a > b ? a : b;
 }
 
 bd_status bd_verify_attn_q(const bd_qkv_desc* kv, const uint16_t* q, int32_t num_q_heads, int32_t gamma, float scale,

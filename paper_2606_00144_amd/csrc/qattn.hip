@@ -18,7 +18,7 @@
 // (two workgroups) convert and multiply: 32 heads x 64 sequences of 4 bits in pages run at 6.0 to 6.25 TB/s (a bare
 // read reaches 6.05), 16K x 8 with 24 rows at 5.7 in the loop (4 bits: MFMA 17%, VALU 40% busy) and 36 us in all,
 // 8 bits at 5.3 and 52 us.  A prologue takes 2 us, the four waves' merge 1.3, a level of records 2.5.  Rows beyond 32
-// are another block, which reads and converts again.  The query rows lie in LDS too: of rows in registers the
+// (48 in long streams) are another block, which reads and converts again.  The query rows lie in LDS too: of rows in registers the
 // compiler waited for all loads at their first use, in every turn of the loop.  Nothing is kept in scratch memory: a
 // wave's first access to it takes 2 to 15 us.
 //
@@ -79,8 +79,9 @@ constexpr int kRing = 2;                       // tile slots of a wave
 constexpr int kMaxBlocks = 512;                // workgroups of a launch
 template <int BITS, int NT, int ROWS>
 struct Config {
-  static constexpr int kPerCu = BITS == 8 || NT == 2 ? 2 : 3;
-  static constexpr int kTab = ROWS == kQContiguous ? 4 : ROWS == kQPages ? 448 : BITS == 8 || NT == 2 ? 1024 : 2048;
+  static constexpr int kPerCu = BITS == 8 || NT > 1 ? 2 : 3;
+  static constexpr int kPart = NT == 3 ? 1 : NT;       // row tiles whose states meet in LDS at a time
+  static constexpr int kTab = ROWS == kQContiguous ? 4 : ROWS == kQPages ? (NT == 3 ? 256 : 448) : BITS == 8 || NT > 1 ? 1024 : 2048;
 };
 
 template <int BITS, int NT, int ROWS>
@@ -88,7 +89,7 @@ struct Smem {
   alignas(16) uint32_t tab[Config<BITS, NT, ROWS>::kTab];
   union {
     alignas(64) uint8_t ring[kWaves][kRing][Tile<BITS>::kBytes];
-    float o[kWaves][16 * NT][kD + 4];          // the waves' states, when they merge
+    float o[kWaves][16 * Config<BITS, NT, ROWS>::kPart][kD + 4];   // the waves' states, when they merge
   } u;
   union {
     alignas(64) uint8_t q[16 * NT][kD * 2];    // query rows, chunk c (16 bytes) of row r at position c ^ k_swizzle(r % 16)
@@ -647,8 +648,10 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       if (ROWS != kQContiguous && c0 < tn) __syncthreads();   // the table is filled again
     }
 
-    // ---- the four waves' states, through LDS.  Thread -> row r and the kPer outputs from d0 on
-    constexpr int kPer = kRows * kD / kThreads;            // 8 or 16
+    // ---- the four waves' states, through LDS, kPart row tiles at a time.  Thread -> row r of a part and the kPer
+    // outputs from d0 on
+    constexpr int kPart = Config<BITS, NT, ROWS>::kPart, kParts = NT / kPart, kPartRows = 16 * kPart;
+    constexpr int kPer = kPartRows * kD / kThreads;        // 8 or 16
     const int tid_m = here(tid), lgm = (tid_m >> 4) & 3, lrm = tid_m & 15;
     const int r = tid_m / (kD / kPer), d0 = (tid_m % (kD / kPer)) * kPer;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the query rows of a piece without keys
@@ -667,43 +670,52 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
         sm.r.stat.l[wave][16 * nt + lrm] = l;
         sm.r.stat.lx[wave][16 * nt + lrm] = lx;
       }
+    }
+    float M[kParts], Ls[kParts], Lx[kParts], acc[kParts][kPer];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float* dst = &sm.u.o[wave][16 * nt + lrm][32 * lgm + 8 * i];
-        *reinterpret_cast<f32x4*>(dst) = f32x4{st.o[nt][0][i], st.o[nt][1][i], st.o[nt][2][i], st.o[nt][3][i]};
-        *reinterpret_cast<f32x4*>(dst + 4) = f32x4{st.o[nt][4][i], st.o[nt][5][i], st.o[nt][6][i], st.o[nt][7][i]};
+    for (int pt = 0; pt < kParts; ++pt) {
+      if (pt > 0) __syncthreads();                         // the part before is read
+#pragma unroll
+      for (int n1 = 0; n1 < kPart; ++n1) {
+        const int nt = pt * kPart + n1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float* dst = &sm.u.o[wave][16 * n1 + lrm][32 * lgm + 8 * i];
+          *reinterpret_cast<f32x4*>(dst) = f32x4{st.o[nt][0][i], st.o[nt][1][i], st.o[nt][2][i], st.o[nt][3][i]};
+          *reinterpret_cast<f32x4*>(dst + 4) = f32x4{st.o[nt][4][i], st.o[nt][5][i], st.o[nt][6][i], st.o[nt][7][i]};
+        }
+      }
+      __syncthreads();
+      const int rr = pt * kPartRows + r;
+      M[pt] = -INFINITY;
+      Ls[pt] = Lx[pt] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M[pt] = fmaxf(M[pt], sm.r.stat.m[w][rr]);
+      const float Mu = M[pt] == -INFINITY ? 0.f : M[pt];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[pt][e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float wt = exp2f(sm.r.stat.m[w][rr] - Mu);
+        Ls[pt] += wt * sm.r.stat.l[w][rr];
+        if constexpr (LSE) Lx[pt] += wt * sm.r.stat.lx[w][rr];
+#pragma unroll
+        for (int e = 0; e < kPer; e += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.u.o[w][r][d0 + e]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[pt][e + k] += wt * x[k];
+        }
+      }
+      if (sm.nan_from[d0 >> 5] <= (gather ? 0x7FFFFFFE : L - p.nq + (rb * kRows + rr) / p.G)) {   // a thread's outputs lie in one block
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[pt][e] = __uint_as_float(0x7FC00000u);
       }
     }
-    __syncthreads();
-    float M = -INFINITY, Ls = 0.f, Lx = 0.f, acc[kPer];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm.r.stat.m[w][r]);
-    const float Mu = M == -INFINITY ? 0.f : M;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) acc[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float wt = exp2f(sm.r.stat.m[w][r] - Mu);
-      Ls += wt * sm.r.stat.l[w][r];
-      if constexpr (LSE) Lx += wt * sm.r.stat.lx[w][r];
-#pragma unroll
-      for (int e = 0; e < kPer; e += 4) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.u.o[w][r][d0 + e]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) acc[e + k] += wt * x[k];
-      }
-    }
-
-    const int row = rb * kRows + r;
-    const bool row_valid = row < p.R;
-    const int jrow = row_valid ? row / p.G : 0;
-    if (sm.nan_from[d0 >> 5] <= (gather ? 0x7FFFFFFE : L - p.nq + jrow)) {         // a thread's outputs lie in one block
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] = __uint_as_float(0x7FC00000u);
-    }
-    const int64_t orow = ((int64_t)s * p.nq + jrow) * p.Hq + g * p.G + (row_valid ? row - jrow * p.G : 0);
-    auto write_final = [&](float Mf, float Lf, float Lxf, const float (&a)[kPer]) {
-      if (!row_valid) return;
+    auto row_valid = [&](int pt) { return rb * kRows + pt * kPartRows + r < p.R; };
+    auto write_final = [&](int pt, float Mf, float Lf, float Lxf, const float (&a)[kPer]) {
+      if (!row_valid(pt)) return;
+      const int row = rb * kRows + pt * kPartRows + r, jrow = row / p.G;
+      const int64_t orow = ((int64_t)s * p.nq + jrow) * p.Hq + g * p.G + (row - jrow * p.G);
       const float inv = Lf == 0.f ? 0.f : 1.f / Lf;        // no visible key: 0
       uint16_t* dst = p.out + orow * kD + d0;
 #pragma unroll
@@ -717,37 +729,39 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
     // ---- pieces of the unit: shares w0 .. w1
     const int w0 = unit0 / chunk, w1 = (unit0 + span - 1) / chunk;
     if (whole || w0 == w1) {
-      write_final(M, Ls, Lx, acc);
+#pragma unroll
+      for (int pt = 0; pt < kParts; ++pt) write_final(pt, M[pt], Ls[pt], Lx[pt], acc[pt]);
     } else {
       const __amdgpu_buffer_rsrc_t rec = make_rsrc(p.part, p.part_bytes);
       // a share leaves at most two records: of a unit that began before it, and of one that goes on after it
       auto at = [&](int w) { return (uint32_t)(2 * (w * p.n_rb + rb) + (w == w0 ? 1 : 0)) * (uint32_t)(kRec * 4); };
-      auto store = [&](int w, float Mr, float Lr, float Lxr, const float (&a)[kPer]) {
-        if (!row_valid) return;
-        if (d0 == 0) store16_coherent(rec, at(w) + 16 * r, f32x4{Mr, Lr, Lxr, 0.f});
+      auto store = [&](int pt, int w, float Mr, float Lr, float Lxr, const float (&a)[kPer]) {
+        if (!row_valid(pt)) return;
+        if (d0 == 0) store16_coherent(rec, at(w) + 16 * (pt * kPartRows + r), f32x4{Mr, Lr, Lxr, 0.f});
 #pragma unroll
         for (int c = 0; c < kPer / 4; ++c)
-          store16_coherent(rec, at(w) + 16 * kRows + 16 * (c * kThreads + tid_m),
+          store16_coherent(rec, at(w) + 16 * kRows + 16 * ((pt * (kPer / 4) + c) * kThreads + tid_m),
                            f32x4{a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]});
       };
       float Mg, Lg, Lxg, ag[kPer];
       // records of shares first, first + step, ..., in that order, a batch of loads at a time
-      auto merge = [&](int first, int count, int step) {
+      auto merge = [&](int pt, int first, int count, int step) {
         Mg = -INFINITY;
         Lg = Lxg = 0.f;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) ag[e] = 0.f;
-        if (!row_valid) return;
-        constexpr int kBatch = NT == 1 ? 8 : 4;            // all loads of a batch are issued before any is used
+        if (!row_valid(pt)) return;
+        constexpr int kBatch = kPer == 8 ? 8 : 4;            // all loads of a batch are issued before any is used
         for (int k0 = 0; k0 < count; k0 += kBatch) {
           f32x4 sv[kBatch], ov[kBatch][kPer / 4];
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) {
             // past the last record: an address past the buffer, which reads as zeros
             const uint32_t a = k0 + u < count ? at(first + (k0 + u) * step) : p.part_bytes;
-            sv[u] = load16_coherent(rec, a + 16 * r);
+            sv[u] = load16_coherent(rec, a + 16 * (pt * kPartRows + r));
 #pragma unroll
-            for (int c = 0; c < kPer / 4; ++c) ov[u][c] = load16_coherent(rec, a + 16 * kRows + 16 * (c * kThreads + tid_m));
+            for (int c = 0; c < kPer / 4; ++c)
+              ov[u][c] = load16_coherent(rec, a + 16 * kRows + 16 * ((pt * (kPer / 4) + c) * kThreads + tid_m));
           }
           float mb = Mg;
 #pragma unroll
@@ -792,20 +806,25 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       const int grp = (share - w0) / kGroup;
       const int g0 = two ? w0 + grp * kGroup : w0;
       const int gn = two ? (np - grp * kGroup < kGroup ? np - grp * kGroup : kGroup) : np;
-      store(share, M, Ls, Lx, acc);
+#pragma unroll
+      for (int pt = 0; pt < kParts; ++pt) store(pt, share, M[pt], Ls[pt], Lx[pt], acc[pt]);
       // counter lines, each shares x row blocks: whole units, named by their first share; first groups, by the same;
       // other groups, by theirs, in which another unit's first group may begin
       const int region = !two ? 0 : grp == 0 ? 1 : 2;
       if (last_of((region * p.nW + g0) * p.n_rb + rb, gn)) {
-        merge(g0, gn, 1);
-        if (!two) {
-          write_final(Mg, Lg, Lxg, ag);
-        } else {
-          __syncthreads();                                 // the group's first record is read: it is written again
-          store(g0, Mg, Lg, Lxg, ag);
-          if (last_of(w0 * p.n_rb + rb, (np + kGroup - 1) / kGroup)) {
-            merge(w0, (np + kGroup - 1) / kGroup, kGroup);
-            write_final(Mg, Lg, Lxg, ag);
+        for (int pt = 0; pt < kParts; ++pt) {
+          merge(pt, g0, gn, 1);
+          if (!two) {
+            write_final(pt, Mg, Lg, Lxg, ag);
+          } else {
+            __syncthreads();                               // the group's first record is read: it is written again
+            store(pt, g0, Mg, Lg, Lxg, ag);
+          }
+        }
+        if (two && last_of(w0 * p.n_rb + rb, (np + kGroup - 1) / kGroup)) {
+          for (int pt = 0; pt < kParts; ++pt) {
+            merge(pt, w0, (np + kGroup - 1) / kGroup, kGroup);
+            write_final(pt, Mg, Lg, Lxg, ag);
           }
         }
       }
@@ -823,14 +842,15 @@ hipError_t launch_rows(const QAttnParams& p, const QAttnPlan& pl, hipStream_t st
   const dim3 grid((unsigned)pl.nblk), block(kThreads);
   if (pl.rows == kQContiguous) hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQContiguous, LSE>), grid, block, 0, stream, p);
   else if (pl.rows == kQPages) hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQPages, LSE>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQTable, LSE>), grid, block, 0, stream, p);
+  else if constexpr (NT < 3) hipLaunchKernelGGL((qattn_kernel<BITS, NT, kQTable, LSE>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
 
 template <int BITS>
 hipError_t launch_bits(const QAttnParams& p, const QAttnPlan& pl, hipStream_t stream) {
   if (pl.nt == 1) return p.lse ? launch_rows<BITS, 1, true>(p, pl, stream) : launch_rows<BITS, 1, false>(p, pl, stream);
-  return p.lse ? launch_rows<BITS, 2, true>(p, pl, stream) : launch_rows<BITS, 2, false>(p, pl, stream);
+  if (pl.nt == 2) return p.lse ? launch_rows<BITS, 2, true>(p, pl, stream) : launch_rows<BITS, 2, false>(p, pl, stream);
+  return p.lse ? launch_rows<BITS, 3, true>(p, pl, stream) : launch_rows<BITS, 3, false>(p, pl, stream);
 }
 
 }  // namespace
@@ -839,11 +859,15 @@ QAttnPlan plan_qattn(int S, int Hkv, int Hq, int nq, int64_t entries, bool gathe
   QAttnPlan pl{};
   const int64_t R = (int64_t)nq * (Hq / Hkv);
   pl.R = (int)(R < (1 << 30) ? R : (1 << 30));
-  pl.nt = R <= 16 ? 1 : 2;
-  pl.n_rb = (pl.R + 16 * pl.nt - 1) / (16 * pl.nt);
   pl.rows = gather ? kQTable : !paged ? kQContiguous : page_size % 16 == 0 ? kQPages : kQTable;
   const int64_t span = (entries + kTile - 1) / kTile;
   const int64_t tiles = (int64_t)S * Hkv * (span > kMinSpan ? span : kMinSpan);
+  // Blocks of 48 rows where they are fewer by more than a quarter (their turns take about 4/3 as long) and the stream is
+  // long enough for their longer merges.  With 48 and 32, 4 bits: 36 rows, 8 x 8 heads of 16K, 48 and 57 us (8 bits 58
+  // and 70); 72 rows 71 and 80; 48 rows, 16 x 8 of 1K to 4K, 29 and 32; but 45 rows, 3 x 8 of 12.5K, 33 and 29.
+  const bool three = pl.rows != kQTable && 4 * ((R + 47) / 48) < 3 * ((R + 31) / 32) && tiles >= 24 * kMaxBlocks;
+  pl.nt = R <= 16 ? 1 : three ? 3 : 2;
+  pl.n_rb = (pl.R + 16 * pl.nt - 1) / (16 * pl.nt);
   int64_t nW = (int64_t)S * Hkv * (((span > kMinSpan ? span : kMinSpan) + kMinSpan - 1) / kMinSpan);   // whole shares a unit
   const int64_t most = kMaxBlocks / pl.n_rb > 1 ? kMaxBlocks / pl.n_rb : 1;
   if (nW > most) nW = most;

@@ -216,6 +216,36 @@ def test_verify_many_sequences(bits, S):
 
 
 @BITS
+@pytest.mark.parametrize("page", [0, 16, 24])
+@pytest.mark.parametrize("Hq,Hkv,gamma", [(8, 1, 4), (8, 2, 8), (16, 2, 8)])
+def test_verify_more_than_32_rows(bits, page, Hq, Hkv, gamma):
+    # 40, 36 and 72 rows a KV head, in a capacity that calls for blocks of three row tiles (24-row pages: of two)
+    S, have, cap = 6, 5000, 65536
+    lens = [have, 33, 0, 1200, 700, 64]
+    cache, kb, vb = make_cache(S, Hkv, have, bits, lens, Hq + gamma)
+    q = rows((S, gamma + 1, Hq, 128), Hq + gamma + 5)
+    table = None
+    if page:
+        pool, table = to_pages(cache, lens, page, 6)
+        cap = cap // page * page
+        wide = np.full((S, cap // page), -1, np.int32)
+        wide[:, :table.shape[1]] = table
+        dev, table = to_dev(pool), i32_dev(wide)
+    else:
+        dev = bd.quant_kv_empty(S, Hkv, cap, bits)
+        for b, h in zip(dev, to_dev(cache)):
+            b.fill_(255)
+            b[:, :, :have] = h
+    case(f"verify_q many rows bits={bits} heads={Hq}/{Hkv} gamma={gamma} page={page}")
+    nb = bd.lib().bd_verify_attn_q_workspace_bytes(S, Hkv, Hq, gamma, cap)
+    out, lse = bd.bd_verify_attn_q(dev, bf16_dev(q), i32_dev(lens), return_lse=True, page_table=table, max_seq_len=cap,
+                                   workspace=poison_workspace(nb))
+    torch.cuda.synchronize()
+    ref = lambda q, k, v: O.verify_attn(k, v, q, lens, gamma)
+    check_out(out, lse, *ref(q, kb, vb), kb, vb, q, ref, have, "many rows")
+
+
+@BITS
 @pytest.mark.parametrize("S,Hkv,top", [(24, 4, 2600), (9, 8, 900), (60, 2, 700), (3, 2, 5000), (40, 4, 300)])
 def test_verify_ragged_batches(bits, S, Hkv, top):
     # units with shares of their own of every length, shares of two units, short units that are not cut
