@@ -336,8 +336,7 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lg = lane >> 4, lr = lane & 15;
-  const int bid = xcd_remap(blockIdx.x + fetch_args(p), gridDim.x);
-  const int share = bid / p.n_rb, rb = bid - share * p.n_rb;
+  const int block = blockIdx.x + fetch_args(p);
   const bool gather = p.idx != nullptr;
 
   // ---- the share: [begin, end) of the stream, its first piece in sequence s.  The stream is counted in tiles and cut
@@ -372,9 +371,12 @@ __global__ __launch_bounds__(kThreads, (Config<BITS, NT, ROWS>::kPerCu)) void qa
       chunk = 1;
     }
   }
-  const int64_t begin64 = (int64_t)share * chunk;
-  if (begin64 >= total) return;
-  const int begin = (int)begin64;
+  // the workgroups that have a share are the first of the launch, spread evenly over the XCDs
+  const int working = (total + chunk - 1) / chunk * p.n_rb;
+  if (block >= working) return;
+  const int bid = xcd_remap(block, working);
+  const int share = bid / p.n_rb, rb = bid - share * p.n_rb;
+  const int begin = share * chunk;
   const int end = total - begin < chunk ? total : begin + chunk;
   int s = 0, before = 0;                       // tiles of the sequences before s
   for (int s0 = 0, acc = 0; s0 < p.S; s0 += kWave) {
