@@ -607,10 +607,12 @@ class QuantKV(_QuantTensors):
         dev = k.get_device()
         if v.get_device() != dev or ks.get_device() != dev or vs.get_device() != dev:
             raise BdError(BD_ERR_INVALID_ARG, "a cache's tensors must be on one device")
+        self._shared_rows = any(sh[i] > 1 and st[i] == 0 for i in (0, 1, 2))
         self._geometry = (w // 16, n0, hkv, n2, st[0] // w, st[1] // w, st[2] // w, dev)
         return self._geometry
 
     _geometry = None
+    _shared_rows = False     # an expanded cache, which can be read but not appended to
 
 
 def quant_kv_empty(n: int, num_kv_heads: int, rows: int, bits: int, device="cuda") -> QuantKV:
@@ -626,6 +628,8 @@ _capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.
 
 def _qkv(cache, seq_lens, page_table=None, max_seq_len=None):
     """The bytes of a QkvDesc for these tensors (checked), and its (num_seqs, num_kv_heads, max_seq_len, device)."""
+    if not isinstance(cache, QuantKV):
+        raise BdError(BD_ERR_INVALID_ARG, "the cache must be a QuantKV")
     bits, n0, hkv, n2, s0, s1, s2, dev = cache._geometry or cache.geometry()
     ls = seq_lens.shape
     if not (seq_lens.dtype == _I32T and len(ls) == 1 and seq_lens.is_contiguous()):
@@ -683,6 +687,8 @@ def bd_cache_append_q(cache: QuantKV, seq_lens: torch.Tensor, k_new: torch.Tenso
     seq_lens[s] .. (the first counts[s] of them with counts int32 [S]); seq_lens (and, with the sparse list
     idx [S, Hkv, ld] / nsel [S], the list) advance in place."""
     kv, S, hkv, _, dev = _qkv(cache, seq_lens, page_table, max_seq_len)
+    if cache._shared_rows:
+        raise BdError(BD_ERR_INVALID_ARG, "rows of an expanded cache overlap: it cannot be appended to")
     ns = k_new.shape
     if not (k_new.dtype == _BF16 and len(ns) == 4 and k_new.is_contiguous() and v_new.shape == ns and v_new.is_contiguous()
             and v_new.dtype == _BF16 and ns[0] == S and ns[2] == hkv and ns[3] == HEAD_DIM):
@@ -721,6 +727,7 @@ def bd_cache_read_q(cache: QuantKV, seq_lens: torch.Tensor, n: int, *, first: Op
     st = ko.stride()
     if outputs is not None:
         _require(ko.dtype == _BF16 and ko.shape == shape and st[3] == 1, "k output must be bf16 [S,Hkv,n,128]")
+        _require(all(d == 1 or t > 0 for d, t in zip(shape, st)), "output rows must not overlap")
         _require(vo is None or (vo.dtype == _BF16 and vo.shape == shape and vo.stride() == st), "v output must match k's")
     _here(dev, seq_lens, first, ko, vo, page_table)
     _check((_packed or _packed_lib()).bd_cache_read_q(kv, _ptr(first), n, ko.data_ptr(), _ptr(vo), st[0], st[1], st[2],

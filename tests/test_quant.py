@@ -199,6 +199,9 @@ def test_binding_refusals():
            lambda: bd.bd_sparse_decode_attn_q(c, q.float(), idx, lens, lens), lambda: bd.bd_sparse_decode_attn_q(c, q[:2], idx, lens, lens),
            lambda: bd.bd_sparse_decode_attn_q(c, q, idx[:, :1].contiguous(), lens, lens), lambda: bd.bd_sparse_decode_attn_q(c, q, idx.long(), lens, lens),
            lambda: bd.bd_sparse_decode_attn_q(c, q, idx, lens[:2], lens), lambda: bd.bd_sparse_decode_attn_q(c, q, idx, lens, lens, out=out),
+           lambda: bd.bd_cache_read_q(c, lens, 4, outputs=(out[:, :, :1].expand(3, 2, 4, 128), None)),
+           lambda: bd.bd_cache_append_q(tuple(c), lens, rows_, rows_),
+           lambda: bd.bd_cache_append_q(bd.QuantKV(*[b[:1].expand(3, -1, -1, -1) for b in c]), lens, rows_, rows_),
            lambda: bd.bd_verify_attn_q(c, q, lens), lambda: bd.bd_verify_attn_q(c, q[:2, None].contiguous(), lens),
            lambda: bd.bd_verify_attn_q(c, q[:, None, :, :64].contiguous(), lens)]
     for i, call in enumerate(bad):
